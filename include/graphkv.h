@@ -258,6 +258,110 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
                                 const void *Qw, void *Kout, void *Vout, int32_t *idx,
                                 float *scores_out, void *stream);
 
+/*
+ * A paged cache, and attention over it.
+ *
+ * Where the calls above take a prompt's cache as one matrix a head, these keep the
+ * rows of many sequences, evicted or whole, in the pages of a pool: what
+ * graphkv_compress leaves is written to pages (graphkv_cache_write), the tokens that
+ * are generated behind it are appended the same way, graphkv_attend computes the
+ * attention of new tokens over what a sequence holds, and graphkv_cache_read lays
+ * rows of a sequence out again, as graphkv_compress takes them.  One call handles one
+ * layer.
+ *
+ *   pools     [n_pages, H_kv, page_tokens, d], one for keys and one for values: rows
+ *             of p->dtype (GRAPHKV_PAGES_PLAIN) or 8-bit codes (see below)
+ *   scales    [n_pages, H_kv, page_tokens] fp32, of the codes: a row's values are its
+ *             codes times its scale (NULL with GRAPHKV_PAGES_PLAIN)
+ *   table     [n_seqs, table_pages] int32: entry i of sequence s is the page that holds
+ *             its positions i * page_tokens and on
+ *   seq_len   [n_seqs] int32: tokens of a sequence, new ones included
+ *   row_start [n_seqs + 1] int32, ascending: rows row_start[s] .. row_start[s+1]-1 of
+ *             the row tensors (K, V, Q, out, lse) belong to sequence s and are its LAST
+ *             tokens.  With n of them, row row_start[s] + i has position
+ *             seq_len[s] - n + i.
+ * table, seq_len and row_start are DEVICE arrays, read when the kernels run: a captured
+ * graph serves batches whose lengths change from replay to replay.  Rows before
+ * row_start[0] and from row_start[n_seqs] on belong to no sequence: none of their
+ * outputs is written (a batch padded to a fixed number of rows).
+ *
+ * No content of these arrays makes a call touch memory outside the tensors.  Lengths
+ * are cut to 0 .. table_pages * page_tokens, row numbers to 0 .. n_rows and to
+ * max_rows a sequence.  A position whose page number is not one of 0 .. n_pages-1, and
+ * a row whose position is negative (more rows than tokens), has no place: it is not
+ * written, it reads as zeros, nothing sees it.
+ *
+ * 8-bit forms keep a row of a head with one scale: the least power of two 2^k with
+ * max|x| <= 448 * 2^k and codes in e4m3 (OCP, no infinities), or max|x| / 127 rounded
+ * to 32 bits and integer codes; codes are the values nearest to x / scale, ties to the even
+ * one.  Rows with max|x| < 2^-100 have scale and codes 0.  Infinities and NaN in rows
+ * to be written are not supported with them.
+ */
+enum { GRAPHKV_PAGES_PLAIN = 0, GRAPHKV_PAGES_FP8 = 1, GRAPHKV_PAGES_INT8 = 2 };
+
+typedef struct graphkv_paged_params {
+    int32_t n_kv_heads;    /* H_kv >= 1                                                  */
+    int32_t n_q_heads;     /* H_q, a multiple of H_kv (attend only)                      */
+    int32_t head_dim;      /* d, a multiple of 8 (16 with 8-bit pages), <= 512           */
+    int32_t dtype;         /* GRAPHKV_FP32 / GRAPHKV_BF16: type of the rows K, V, Q, out */
+    int32_t page_format;   /* GRAPHKV_PAGES_*                                            */
+    int32_t page_tokens;   /* tokens a page holds, a power of two, <= 65536              */
+    int32_t n_pages;       /* n_pages * H_kv * page_tokens < 2^31                        */
+    int32_t n_seqs;        /* 0 .. 2^20                                                  */
+    int32_t table_pages;   /* >= 1, table_pages * page_tokens <= 2^30                    */
+    int32_t n_rows;        /* rows of the row tensors, 0 .. 2^26                         */
+    int32_t max_rows;      /* no sequence has more rows than this; 0: n_rows             */
+    float   softmax_scale; /* attend: 0 selects 1/sqrt(d)                                */
+    int32_t impl;          /* GRAPHKV_IMPL_*: GENERIC forces the scalar kernel (attend)  */
+    int64_t row_stride;    /* elements between rows and between heads of K and V (write, */
+    int64_t head_stride;   /*   read) or Q (attend); both 0: packed [n_rows, heads, d].  */
+    int64_t out_row_stride;   /* the same for the output of attend.  Strides are         */
+    int64_t out_head_stride;  /*   multiples of 16 bytes; outputs must not overlap       */
+} graphkv_paged_params;
+
+/*
+ * Writes rows to the places of their tokens, encoded where the pages hold codes.
+ *   K, V            [n_rows, H_kv, d] with the params' strides, in
+ *   Kpages, Vpages  in/out: places of other tokens keep what they hold
+ *   Kscale, Vscale  in/out, with 8-bit pages
+ * No two rows of a call may have the same place (sequences that share pages must not
+ * write to them): such a place would hold a mixture of their rows.
+ */
+int32_t graphkv_cache_write(const graphkv_paged_params *p, const void *K, const void *V, void *Kpages,
+                            void *Vpages, float *Kscale, float *Vscale, const int32_t *table,
+                            const int32_t *seq_len, const int32_t *row_start, void *stream);
+
+/*
+ * The reverse: K, V [n_rows, H_kv, d] (out, with the params' strides) get the rows' values,
+ * rounded once to p->dtype.  Strides of n_rows * d between heads and d between rows
+ * give the [H_kv, n_rows, d] of the calls above.
+ */
+int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, const void *Vpages,
+                           const float *Kscale, const float *Vscale, const int32_t *table,
+                           const int32_t *seq_len, const int32_t *row_start, void *K, void *V, void *stream);
+
+/*
+ * Causal attention of new tokens over the cache, which already holds their own rows:
+ * a row at position t sees the positions 0 .. t of its sequence,
+ *   out = sum_j softmax_j(<q, k_j> * scale) v_j,   lse = log sum_j exp(<q, k_j> * scale),
+ * with query head i on key-value head i / (H_q / H_kv).  One token a sequence, a few
+ * drafted ones, a chunk of a prompt, or a mixture of these in one call.
+ *   Q    [n_rows, H_q, d] in, out [n_rows, H_q, d] out, with their strides
+ *   lse  [n_rows, H_q]    out, optional (NULL), fp32
+ *   ws   graphkv_attend_workspace_bytes(p) bytes, 256-byte aligned
+ * Softmax statistics and sums are held in 32 bits; with bf16 rows the weights are
+ * rounded to bf16 for the product with the values.  A row that sees nothing has
+ * out = 0 and lse = -infinity.  What lies in places that a row does not see (later
+ * positions, the rest of a page) has no influence on it, whatever its bits.
+ * Results are deterministic; a sequence's may differ in their last bits with the
+ * sequences beside it, which change where its sums are cut.
+ */
+size_t graphkv_attend_workspace_bytes(const graphkv_paged_params *p);
+int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void *Kpages, const void *Vpages,
+                       const float *Kscale, const float *Vscale, const int32_t *table,
+                       const int32_t *seq_len, const int32_t *row_start, void *out, float *lse, void *ws,
+                       size_t ws_bytes, void *stream);
+
 /* Host string for a return code (static storage). */
 const char *graphkv_strerror(int32_t code);
 
@@ -285,7 +389,10 @@ enum {
     /* later rounds when neighbour lists are kept: source selection, and the bound, filter and
      * select passes over the few sources that have no list yet */
     GRAPHKV_K_TOPK_SOURCES_LATER, GRAPHKV_K_COSINE_BOUND_NEW, GRAPHKV_K_COSINE_FILTER_NEW,
-    GRAPHKV_K_NBR_SELECT_LATER, GRAPHKV_N_KERNELS
+    GRAPHKV_K_NBR_SELECT_LATER,
+    /* paged cache */
+    GRAPHKV_K_CACHE_WRITE, GRAPHKV_K_CACHE_READ, GRAPHKV_K_ATTEND_GENERIC, GRAPHKV_K_ATTEND_FEW,
+    GRAPHKV_K_ATTEND_MANY, GRAPHKV_K_ATTEND_JOIN, GRAPHKV_N_KERNELS
 };
 int32_t graphkv_profile_begin(void);
 int32_t graphkv_profile_end(double *ms, int64_t *launches);

@@ -23,14 +23,16 @@ SIGNAL_DECAY, SIGNAL_ENHANCED, SIGNAL_EVICTED = 0, 1, 2
 IMPL_AUTO, IMPL_GENERIC = 0, 1
 EDGES_KK, EDGES_KV, EDGES_VV = 0, 1, 2
 SCORER_ATTENTION, SCORER_KNORM = 0, 1
+PAGES_PLAIN, PAGES_FP8, PAGES_INT8 = 0, 1, 2
 
 EXPORTS = ("graphkv_workspace_bytes", "graphkv_score", "graphkv_score_knorm", "graphkv_propagate",
            "graphkv_select", "graphkv_compress", "graphkv_strerror", "graphkv_uses_mfma",
            "graphkv_profile_begin", "graphkv_profile_end", "graphkv_kernel_name",
            "graphkv_workspace_bytes_batched", "graphkv_compress_batched", "graphkv_propagate_edges",
-           "graphkv_compress_static", "graphkv_select_workspace_bytes")
+           "graphkv_compress_static", "graphkv_select_workspace_bytes", "graphkv_cache_write", "graphkv_cache_read",
+           "graphkv_attend", "graphkv_attend_workspace_bytes")
 STATIC_SCRATCH_BYTES = 64 << 20
-N_KERNELS = 23
+N_KERNELS = 29
 
 
 class GraphKVError(RuntimeError):
@@ -85,6 +87,48 @@ class Params:
         return torch.float32 if self.dtype == FP32 else torch.bfloat16
 
 
+class _CPagedParams(ctypes.Structure):
+    _fields_ = [
+        ("n_kv_heads", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_format", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("table_pages", ctypes.c_int32),
+        ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("impl", ctypes.c_int32), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+    ]
+
+
+@dataclass
+class PagedParams:
+    """Mirror of graphkv_paged_params (see include/graphkv.h for the constraints); strides come from the tensors."""
+    n_kv_heads: int
+    head_dim: int
+    page_tokens: int
+    n_pages: int
+    n_seqs: int
+    table_pages: int
+    n_rows: int
+    n_q_heads: int = 0
+    max_rows: int = 0
+    dtype: int = BF16
+    page_format: int = PAGES_PLAIN
+    softmax_scale: float = 0.0
+    impl: int = IMPL_AUTO
+
+    def c(self, rows=(0, 0), out=(0, 0)) -> _CPagedParams:
+        return _CPagedParams(self.n_kv_heads, self.n_q_heads, self.head_dim, self.dtype, self.page_format, self.page_tokens,
+                             self.n_pages, self.n_seqs, self.table_pages, self.n_rows, self.max_rows, self.softmax_scale,
+                             self.impl, *rows, *out)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == FP32 else torch.bfloat16
+
+    @property
+    def page_dtype(self):
+        return {PAGES_FP8: torch.float8_e4m3fn, PAGES_INT8: torch.int8}.get(self.page_format, self.torch_dtype)
+
+
 _lib = None
 
 
@@ -123,6 +167,15 @@ def load_library() -> ctypes.CDLL:
     lib.graphkv_workspace_bytes_batched.argtypes = [pp, i32]
     lib.graphkv_compress_batched.restype = i32
     lib.graphkv_compress_batched.argtypes = [pp, i32, ctypes.POINTER(i32), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    gp = ctypes.POINTER(_CPagedParams)
+    lib.graphkv_cache_write.restype = i32
+    lib.graphkv_cache_write.argtypes = [gp] + [vp] * 10
+    lib.graphkv_cache_read.restype = i32
+    lib.graphkv_cache_read.argtypes = [gp] + [vp] * 10
+    lib.graphkv_attend_workspace_bytes.restype = sz
+    lib.graphkv_attend_workspace_bytes.argtypes = [gp]
+    lib.graphkv_attend.restype = i32
+    lib.graphkv_attend.argtypes = [gp] + [vp] * 11 + [sz, vp]
     lib.graphkv_strerror.restype = ctypes.c_char_p
     lib.graphkv_strerror.argtypes = [i32]
     lib.graphkv_profile_begin.restype = i32
@@ -344,6 +397,107 @@ def graphkv_compress_batched(p: Params, n_layers: int, budgets, Kc, Vc, Qw, Kout
         _arg(scores_out, "scores_out", torch.float32, n_layers * p.n_kv_heads * p.n_prefix, optional=True),
         wp, wn, _stream()))
     return Kout, Vout, idx
+
+
+# ---- paged cache ----
+
+def _rows_arg(p: PagedParams, t, name: str, heads: int, dev):
+    """(address, strides) of a tensor [n_rows, heads, d], any strides that keep a row's d values together."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != dev:
+        raise GraphKVError(f"{name} must be a tensor on the pools' device")
+    if t.dtype != p.torch_dtype:
+        raise GraphKVError(f"{name} must have dtype {p.torch_dtype}, got {t.dtype}")
+    if t.shape != (p.n_rows, heads, p.head_dim):
+        raise GraphKVError(f"{name} must have shape {(p.n_rows, heads, p.head_dim)}, got {tuple(t.shape)}")
+    row, head, one = t.stride()
+    # (the stride of a dimension of one entry is never used; it is told as what a packed tensor has)
+    if heads == 1:
+        head = p.head_dim
+    if p.n_rows <= 1:
+        row = heads * head
+    unit = 16 // t.element_size()
+    if t.numel() and (one != 1 or row < p.head_dim or head < p.head_dim or row % unit or head % unit):
+        raise GraphKVError(f"{name}: rows of {p.head_dim} values together, strides in multiples of 16 bytes; got strides {t.stride()}")
+    return t.data_ptr(), (row, head) if t.numel() else (0, 0)
+
+
+def _pool_args(p: PagedParams, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale):
+    """Addresses of what the calls on a paged cache share, checked; the device they live on."""
+    rows = p.n_pages * p.n_kv_heads * p.page_tokens
+    coded = p.page_format != PAGES_PLAIN
+    told = ((Kpages, "Kpages", p.page_dtype, rows * p.head_dim), (Vpages, "Vpages", p.page_dtype, rows * p.head_dim),
+            (Kscale if coded else None, "Kscale", torch.float32, rows), (Vscale if coded else None, "Vscale", torch.float32, rows),
+            (table, "table", torch.int32, p.n_seqs * p.table_pages), (seq_len, "seq_len", torch.int32, p.n_seqs),
+            (row_start, "row_start", torch.int32, p.n_seqs + 1))
+    at = [_arg(t, name, dtype, n, optional=not coded and name in ("Kscale", "Vscale")) for t, name, dtype, n in told]
+    dev = Kpages.device
+    if any(t is not None and t.device != dev for t, *_ in told):
+        raise GraphKVError("the pools, scales, table, seq_len and row_start must be on one device")
+    return at, dev
+
+
+def _new_rows(p: PagedParams, heads: int, dev):
+    return torch.empty((p.n_rows, heads, p.head_dim), dtype=p.torch_dtype, device=dev)
+
+
+def _call_on(dev, f, *args):
+    """Calls f(*args, stream) with the tensors' device as the current one, on its current stream."""
+    if dev.index is None or dev.index == torch.cuda.current_device():
+        return f(*args, _stream())
+    with torch.cuda.device(dev):
+        return f(*args, _stream())
+
+
+def graphkv_cache_write(p: PagedParams, K, V, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None):
+    """Writes rows K, V [n_rows, H_kv, d] (views with strides are taken as they are) to the places of their tokens.
+    Kpages, Vpages [n_pages, H_kv, page_tokens, d] of p.page_dtype, scales [n_pages, H_kv, page_tokens] fp32."""
+    at, dev = _pool_args(p, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale)
+    kp, ks = _rows_arg(p, K, "K", p.n_kv_heads, dev)
+    vp, vs = _rows_arg(p, V, "V", p.n_kv_heads, dev)
+    if ks != vs:
+        raise GraphKVError(f"K and V must have the same strides, got {ks} and {vs}")
+    _check(_call_on(dev, load_library().graphkv_cache_write, ctypes.byref(p.c(ks)), kp, vp, *at))
+
+
+def graphkv_cache_read(p: PagedParams, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None, K=None, V=None):
+    """(K, V): the rows' values, [n_rows, H_kv, d] (allocated if None; rows of no sequence stay as they are)."""
+    at, dev = _pool_args(p, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale)
+    K = _new_rows(p, p.n_kv_heads, dev) if K is None else K
+    V = torch.empty_strided(K.shape, K.stride(), dtype=K.dtype, device=dev) if V is None else V
+    kp, ks = _rows_arg(p, K, "K", p.n_kv_heads, dev)
+    vp, vs = _rows_arg(p, V, "V", p.n_kv_heads, dev)
+    if ks != vs:
+        raise GraphKVError(f"K and V must have the same strides, got {ks} and {vs}")
+    pools, scales, batch = at[:2], at[2:4], at[4:]
+    _check(_call_on(dev, load_library().graphkv_cache_read, ctypes.byref(p.c(ks)), *pools, *scales, *batch, kp, vp))
+    return K, V
+
+
+def graphkv_attend_workspace_bytes(p: PagedParams) -> int:
+    return int(load_library().graphkv_attend_workspace_bytes(ctypes.byref(p.c())))
+
+
+def alloc_attend_workspace(p: PagedParams, device="cuda") -> torch.Tensor:
+    return torch.empty(graphkv_attend_workspace_bytes(p), dtype=torch.uint8, device=device)
+
+
+def graphkv_attend(p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None, out=None,
+                   lse=None, ws=None):
+    """out [n_rows, H_q, d] (allocated if None): causal attention of the rows Q over their sequences' cached tokens.
+    lse: an fp32 tensor [n_rows, H_q] that gets the logarithms of the softmax sums."""
+    at, dev = _pool_args(p, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale)
+    qp, qs = _rows_arg(p, Q, "Q", p.n_q_heads, dev)
+    out = _new_rows(p, p.n_q_heads, dev) if out is None else out
+    op, os_ = _rows_arg(p, out, "out", p.n_q_heads, dev)
+    lp = _arg(lse, "lse", torch.float32, p.n_rows * p.n_q_heads, optional=True)
+    cp = p.c(qs, os_)
+    if ws is None:
+        ws = torch.empty(load_library().graphkv_attend_workspace_bytes(ctypes.byref(cp)), dtype=torch.uint8, device=dev)
+    wp = _arg(ws, "ws", torch.uint8, 0)
+    if ws.device != dev or (lse is not None and lse.device != dev):
+        raise GraphKVError("lse and ws must be on the pools' device")
+    _check(_call_on(dev, load_library().graphkv_attend, ctypes.byref(cp), qp, *at, op, lp, wp, ws.numel()))
+    return out
 
 
 def graphkv_profile_begin():

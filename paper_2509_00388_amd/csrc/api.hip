@@ -1,6 +1,7 @@
 // C ABI of the library (include/graphkv.h): argument checks, workspace carving
 // and the order in which the kernels of one layer call are enqueued.
 #include "../../include/graphkv.h"
+#include "attend.hpp"
 #include "kernels.hpp"
 
 #include <math.h>
@@ -269,7 +270,7 @@ const char *const kKernelNames[GRAPHKV_N_KERNELS] = {
     "decay", "topk_final", "gather", "generic_logits", "generic_votes", "generic_cosine",
     "knorm", "copy", "cosine_bound", "cosine_filter", "nbr_select",
     "redo_rows", "match_sources", "topk_sources_later", "cosine_bound_new", "cosine_filter_new",
-    "nbr_select_later"};
+    "nbr_select_later", "cache_write", "cache_read", "attend_generic", "attend_few", "attend_many", "attend_join"};
 
 #define GKV_LAUNCH(id, expr)                                              \
     do {                                                                  \
@@ -289,6 +290,103 @@ const char *const kKernelNames[GRAPHKV_N_KERNELS] = {
         }                                                                 \
         if (err_ != hipSuccess) return GRAPHKV_EHIP;                      \
     } while (0)
+
+// ---- paged cache ----------------------------------------------------------------
+// Constraints of graphkv_paged_params that the calls have in common.
+bool paged_ok(const graphkv_paged_params *p)
+{
+    if (!p) return false;
+    if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return false;
+    if (p->dtype != GRAPHKV_FP32 && p->dtype != GRAPHKV_BF16) return false;
+    if (p->page_format < GRAPHKV_PAGES_PLAIN || p->page_format > GRAPHKV_PAGES_INT8) return false;
+    if (p->head_dim < 8 || p->head_dim > 512 || p->head_dim % (p->page_format == GRAPHKV_PAGES_PLAIN ? 8 : 16)) return false;
+    if (p->page_tokens < 1 || p->page_tokens > 65536 || (p->page_tokens & (p->page_tokens - 1))) return false;
+    if (p->n_pages < 1 || (__int128)p->n_pages * p->n_kv_heads * p->page_tokens > INT32_MAX) return false;
+    if (p->n_seqs < 0 || p->n_seqs > (1 << 20)) return false;
+    if (p->table_pages < 1 || (int64_t)p->table_pages * p->page_tokens > (1 << 30)) return false;
+    if (p->n_rows < 0 || p->n_rows > (1 << 26) || p->max_rows < 0 || p->max_rows > p->n_rows) return false;
+    if (p->impl != GRAPHKV_IMPL_AUTO && p->impl != GRAPHKV_IMPL_GENERIC) return false;
+    return true;
+}
+
+// Strides of a tensor [n_rows, heads, d]; both 0: packed.  `distinct`: no two of its rows may overlap.
+bool take_strides(const graphkv_paged_params *p, int heads, int64_t row_stride, int64_t head_stride, bool distinct, long &row, long &head)
+{
+    const int64_t d = p->head_dim, unit = p->dtype == GRAPHKV_FP32 ? 4 : 8, most = (int64_t)1 << 44;
+    row = row_stride;
+    head = head_stride;
+    if (row == 0 && head == 0) {
+        row = heads * d;
+        head = d;
+        return true;
+    }
+    if (row < d || head < d || row > most || head > most || row % unit || head % unit) return false;
+    return !distinct || heads == 1 || p->n_rows <= 1 || row >= (heads - 1) * head + d || head >= (p->n_rows - 1) * row + d;
+}
+
+PagedBatch batch_of(const graphkv_paged_params *p, const int32_t *table, const int32_t *seq_len, const int32_t *row_start)
+{
+    PagedBatch b{};
+    b.table = table;
+    b.seq_len = seq_len;
+    b.row_start = row_start;
+    b.n_seqs = p->n_seqs;
+    b.table_pages = p->table_pages;
+    b.n_pages = p->n_pages;
+    b.n_rows = p->n_rows;
+    b.max_rows = p->max_rows ? p->max_rows : p->n_rows;
+    b.H = p->n_kv_heads;
+    b.d = p->head_dim;
+    b.page_shift = __builtin_ctz((unsigned)p->page_tokens);
+    return b;
+}
+
+bool batch_pointers_ok(const graphkv_paged_params *p, const void *Kpages, const void *Vpages, const float *Kscale,
+                       const float *Vscale, const int32_t *table, const int32_t *seq_len, const int32_t *row_start)
+{
+    const bool plain = p->page_format == GRAPHKV_PAGES_PLAIN;
+    auto aligned = [](const void *ptr, uintptr_t n) { return ptr && ((uintptr_t)ptr & (n - 1)) == 0; };
+    return aligned(Kpages, 16) && aligned(Vpages, 16) && (plain || (aligned(Kscale, 4) && aligned(Vscale, 4))) &&
+           aligned(table, 4) && aligned(seq_len, 4) && aligned(row_start, 4);
+}
+
+// Which kernels graphkv_attend launches, and what they leave in its workspace.
+struct AttendPlan {
+    int G;
+    bool generic, few, many;
+    FewPlan fp;
+    ManyPlan mp;
+    size_t many_off, total;
+};
+
+bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
+{
+    if (!paged_ok(p)) return false;
+    if (p->n_q_heads < p->n_kv_heads || p->n_q_heads > 65535 || p->n_q_heads % p->n_kv_heads) return false;
+    if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return false;
+    A = AttendPlan{};
+    A.G = p->n_q_heads / p->n_kv_heads;
+    A.generic = p->impl == GRAPHKV_IMPL_GENERIC || !attend_mfma_applies(p->head_dim);
+    const PagedBatch b = batch_of(p, nullptr, nullptr, nullptr);
+    if (A.generic || b.n_rows == 0 || b.n_seqs == 0) return true;
+    // (key tiles of all sequences and heads, and the workgroups of the largest launch, are counted in 32 bits)
+    const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
+    if (((tokens + 127) / 128) * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
+    if (((int64_t)p->n_rows * A.G / kBlockRows + p->n_seqs) * p->n_kv_heads > INT32_MAX) return false;
+    // Sequences of few rows and of many are different kernels' where both can occur; a batch of one sequence is one or the other.
+    A.many = (int64_t)b.max_rows * A.G > kFewRows;
+    A.few = !A.many || b.n_seqs > 1;
+    if (A.few) {
+        A.fp = few_plan(b, p->dtype, p->page_format, A.G);
+        A.many_off = align_up((size_t)2 * A.fp.n_wg * A.fp.slot_floats * 4);
+    }
+    A.total = A.many_off;
+    if (A.many) {
+        A.mp = many_plan(b, A.G, A.few);
+        if (A.mp.splits > 1) A.total += align_up((size_t)A.mp.blocks * A.mp.splits * b.H * A.mp.slot_floats * 4);
+    }
+    return true;
+}
 
 template <typename T> T *at(void *ws, size_t off) { return reinterpret_cast<T *>((char *)ws + off); }
 
@@ -742,6 +840,86 @@ int32_t graphkv_compress_batched(const graphkv_params *p, int32_t n_layers, cons
     if (!base_ok(p) || n_layers < 1) return GRAPHKV_EINVAL;
     return compress_layers(p, n_layers, group_dims(p, n_layers), budgets, Kc, Vc, Qw, Kout, Vout, idx, scores_out, ws,
                            ws_bytes, stream);
+}
+
+int32_t graphkv_cache_write(const graphkv_paged_params *p, const void *K, const void *V, void *Kpages, void *Vpages,
+                            float *Kscale, float *Vscale, const int32_t *table, const int32_t *seq_len,
+                            const int32_t *row_start, void *stream)
+{
+    long row, head;
+    if (!paged_ok(p) || !take_strides(p, p->n_kv_heads, p->row_stride, p->head_stride, false, row, head)) return GRAPHKV_EINVAL;
+    if (p->n_rows == 0 || p->n_seqs == 0) return GRAPHKV_OK;
+    if (!aligned16(K) || !aligned16(V) || !batch_pointers_ok(p, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start))
+        return GRAPHKV_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    GKV_LAUNCH(GRAPHKV_K_CACHE_WRITE, launch_cache_write(batch_of(p, table, seq_len, row_start), p->dtype, p->page_format, K, V,
+                                                         row, head, Kpages, Vpages, Kscale, Vscale, st));
+    return GRAPHKV_OK;
+}
+
+int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, const void *Vpages, const float *Kscale,
+                           const float *Vscale, const int32_t *table, const int32_t *seq_len, const int32_t *row_start,
+                           void *K, void *V, void *stream)
+{
+    long row, head;
+    if (!paged_ok(p) || !take_strides(p, p->n_kv_heads, p->row_stride, p->head_stride, true, row, head)) return GRAPHKV_EINVAL;
+    if (p->n_rows == 0 || p->n_seqs == 0) return GRAPHKV_OK;
+    if (!aligned16(K) || !aligned16(V) || !batch_pointers_ok(p, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start))
+        return GRAPHKV_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    GKV_LAUNCH(GRAPHKV_K_CACHE_READ, launch_cache_read(batch_of(p, table, seq_len, row_start), p->dtype, p->page_format, Kpages,
+                                                       Vpages, Kscale, Vscale, K, V, row, head, st));
+    return GRAPHKV_OK;
+}
+
+size_t graphkv_attend_workspace_bytes(const graphkv_paged_params *p)
+{
+    AttendPlan A;
+    return plan_attend(p, A) ? A.total : 0;
+}
+
+int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void *Kpages, const void *Vpages,
+                       const float *Kscale, const float *Vscale, const int32_t *table, const int32_t *seq_len,
+                       const int32_t *row_start, void *out, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    AttendPlan A;
+    if (!plan_attend(p, A)) return GRAPHKV_EINVAL;
+    AttendArgs a{};
+    if (!take_strides(p, p->n_q_heads, p->row_stride, p->head_stride, false, a.q_row, a.q_head) ||
+        !take_strides(p, p->n_q_heads, p->out_row_stride, p->out_head_stride, true, a.o_row, a.o_head))
+        return GRAPHKV_EINVAL;
+    if (p->n_rows == 0 || p->n_seqs == 0) return GRAPHKV_OK;
+    if (!aligned16(Q) || !aligned16(out) || (lse && !aligned4(lse)) ||
+        !batch_pointers_ok(p, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start))
+        return GRAPHKV_EINVAL;
+    if (A.total)
+        if (int32_t rc = check_ws(A.total, ws, ws_bytes)) return rc;
+    a.b = batch_of(p, table, seq_len, row_start);
+    a.Q = Q;
+    a.Kpages = Kpages;
+    a.Vpages = Vpages;
+    a.Kscale = Kscale;
+    a.Vscale = Vscale;
+    a.out = out;
+    a.lse = lse;
+    a.G = A.G;
+    a.c = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
+    hipStream_t st = (hipStream_t)stream;
+    if (A.generic) {
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_GENERIC, launch_attend_generic(a, p->dtype, p->page_format, st));
+        return GRAPHKV_OK;
+    }
+    if (A.few) {
+        A.fp.slots = at<float>(ws, 0);
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join_few(a, A.fp, p->dtype, st));
+    }
+    if (A.many) {
+        A.mp.slots = at<float>(ws, A.many_off);
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
+        if (A.mp.splits > 1) GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join_many(a, A.mp, p->dtype, st));
+    }
+    return GRAPHKV_OK;
 }
 
 int32_t graphkv_profile_begin(void)

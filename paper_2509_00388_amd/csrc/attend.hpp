@@ -1,0 +1,112 @@
+// Arguments of the attention kernels (attend.hip, attend_few.hip, attend_many.hip).
+#pragma once
+#include "paged.hpp"
+
+namespace gkv {
+
+// Stacked query rows: the G query heads of a key-value head, token by token (row r is token r / G, head r % G of them).
+struct AttendArgs {
+    PagedBatch b;
+    const void *Q, *Kpages, *Vpages;
+    const float *Kscale, *Vscale;
+    void *out;
+    float *lse;   // [n_rows, H_q] or null
+    int G;
+    float c;      // softmax scale times log2(e)
+    long q_row, q_head, o_row, o_head;   // strides in elements
+};
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kFewRows = 32;   // stacked rows up to which a sequence goes to the kernel for few rows
+
+// The logarithm of the sum from its base-2 parts (m: maximum, l: sum of 2^(x - m), 0 where nothing is seen).
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2; }
+__device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// ---- how work is cut ----------------------------------------------------------------------------------
+// The lengths are known to the device alone, so each workgroup adds up for itself what lies before its share.  `weight(s)` is
+// the work of sequence s in whatever unit; workgroups of 256 threads, `part`: 10 words of LDS.
+template <typename W> __device__ uint32_t weigh(int n_seqs, int of, uint32_t &before, uint32_t *part, W &&weight)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    uint32_t total = 0;
+    before = 0;
+    for (int first = 0; first < n_seqs; first += 256) {
+        const int s = first + tid;
+        const uint32_t w = s < n_seqs ? weight(s) : 0;
+        const uint32_t all = wave_sum_u32(w), some = wave_sum_u32(s < of ? w : 0u);
+        __syncthreads();
+        if (lane == 0) { part[wv] = all; part[4 + wv] = some; }
+        __syncthreads();
+        total += part[0] + part[1] + part[2] + part[3];
+        before += part[4] + part[5] + part[6] + part[7];
+    }
+    return total;
+}
+// The sequence that holds unit `unit` (below the total), and the units before it.
+template <typename W> __device__ int find_unit(int n_seqs, uint32_t unit, uint32_t &before, uint32_t *part, W &&weight)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    uint32_t base = 0;
+    for (int first = 0; first < n_seqs; first += 256) {
+        const int s = first + tid;
+        const uint32_t w = s < n_seqs ? weight(s) : 0;
+        uint32_t total;
+        __syncthreads();
+        const uint32_t at = base + block_scan_add<4>(w, part, lane, wv, total);
+        if (unit >= at && unit < at + w) { part[8] = (uint32_t)s; part[9] = at; }
+        base += total;
+        __syncthreads();
+        if (unit < base) break;
+    }
+    before = part[9];
+    return __builtin_amdgcn_readfirstlane((int)part[8]);
+}
+
+// Few rows: the tiles of all (sequence, key-value head) pairs, one after the other, are cut into equal stretches, one a
+// workgroup (no more stretches than tiles).
+struct FewPlan {
+    int n_wg, tile_keys, slot_rows, slot_floats;
+    float *slots;   // two a workgroup: what its first and its last stretch leave of a pair that others share
+};
+__device__ __forceinline__ bool has_few(const SeqRows &q, int G) { return q.n > 0 && q.n * (long)G <= kFewRows; }
+__device__ __forceinline__ uint32_t few_tiles(const SeqRows &q, const AttendArgs &a, const FewPlan &p)   // of a head
+{
+    return has_few(q, a.G) ? max(1, (q.len + p.tile_keys - 1) / p.tile_keys) : 0;
+}
+// First tile of workgroup w of n, and the workgroup that takes a tile.
+__device__ __forceinline__ uint32_t few_first(uint32_t total, int w, int n) { return (uint32_t)((uint64_t)total * w / n); }
+__device__ __forceinline__ int few_owner(uint32_t total, uint32_t tile, int n)
+{
+    return (int)((((uint64_t)tile + 1) * n - 1) / total);
+}
+
+// Many rows: a workgroup takes a block of kBlockRows stacked rows of a head and one of `splits` equal runs of the key tiles
+// that the block sees.
+constexpr int kBlockRows = 128;
+struct ManyPlan {
+    int blocks;       // at least the blocks of all sequences
+    int splits;
+    int leave_few;    // sequences of few rows are the other kernel's
+    int slot_floats;  // (splits > 1) of a (split, block, head): [kBlockRows, D] sums, [kBlockRows] maxima and sums of weights
+    float *slots;
+};
+__device__ __forceinline__ uint32_t many_blocks(const SeqRows &q, const AttendArgs &a, const ManyPlan &p)
+{
+    return p.leave_few && has_few(q, a.G) ? 0 : (uint32_t)((q.n * (long)a.G + kBlockRows - 1) / kBlockRows);
+}
+
+// ---- launchers ------------------------------------------------------------------------------------------
+bool attend_mfma_applies(int d);   // whether the matrix-core kernels take this head dimension
+FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
+ManyPlan many_plan(const PagedBatch &b, int G, bool leave_few);
+hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st);
+hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_attend_join_few(const AttendArgs &a, const FewPlan &pl, int dtype, hipStream_t st);
+hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_attend_join_many(const AttendArgs &a, const ManyPlan &pl, int dtype, hipStream_t st);
+
+// Head dimension that the matrix-core kernels fill d up to.
+inline int attend_width(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+}  // namespace gkv

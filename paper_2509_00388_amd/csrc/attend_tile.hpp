@@ -1,0 +1,265 @@
+// Pieces of the attention kernels on the matrix cores: operands of v_mfma_f32_32x32x16_bf16 (rows in bf16) and
+// v_mfma_f32_32x32x2_f32 (rows in 32 bits), keys and values on their way through the LDS, the softmax of a tile.
+//
+// The logits are computed with keys as rows and queries as columns, S^T = K Q^T: a lane then owns one query, and
+// of a block of 32 keys it holds 16 (acc_row()), its other half-wave the rest.  The product with the values takes them as
+// they lie: O^T = V^T P^T contracts over keys, and the order of a contraction is free as long as both operands keep to it,
+// so P^T needs no exchange between lanes.  V^T in bf16 comes out of the LDS by gfx950's transposing read.
+#pragma once
+#include "attend.hpp"
+
+namespace gkv {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Row of the 32x32 result in accumulator register i of a lane in half-wave hh (its column is lane % 32).
+__device__ __forceinline__ constexpr int acc_row(int i, int hh) { return 8 * (i >> 2) + 4 * hh + (i & 3); }
+
+__device__ __forceinline__ void add_block(const uint4 &a, const uint4 &b, f32x16 &acc, float)   // 32 bytes a row: 8 values
+{
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void add_block(const uint4 &a, const uint4 &b, f32x16 &acc, uint16_t)   // 32 bytes: 16 values
+{
+    union { uint4 u; bf16x8 v; } x{a}, y{b};
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v, y.v, acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ float other_half_max(float x)   // with the lane 32 places away
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float other_half_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Geometry of a tile of KEYS cached rows of width D (d filled up with zeros to 64, 128 or 256), moved by NT threads.
+// The LDS holds values of type T; a row of keys is padded by 16 bytes, a row of values so that the transposing reads of
+// four keys and 32 dimensions spread over the banks.
+template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
+    static constexpr int kCached = FORM == kPagesPlain ? (int)sizeof(T) : 1;   // bytes of a cached value
+    static constexpr int kPieces = D * kCached / 16;                             // 16-byte pieces of a cached row
+    static constexpr int kPer = KEYS * kPieces / NT;                             // pieces of a thread
+    static constexpr int kRowStep = NT / kPieces;                                // rows between two of its pieces
+    static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + 32;
+    static constexpr int kSteps = D * (int)sizeof(T) / 32;                       // matrix steps of a row of keys
+    static_assert(KEYS * kPieces % NT == 0 && NT % kPieces == 0, "whole rows a turn");
+
+    // Whether a piece holds an infinity or a NaN.
+    __device__ static __forceinline__ bool odd(const uint4 &v)
+    {
+        auto any = [&](auto f) { return f(v.x) || f(v.y) || f(v.z) || f(v.w); };
+        if constexpr (FORM == kPagesFp8) return any([](uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; });
+        if constexpr (FORM == kPagesInt8) return false;
+        if constexpr (sizeof(T) == 4) return any([](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; });
+        return any([](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u; });
+    }
+    // Rows of the tile, of those that this wave moves, that hold one (the pieces of a row lie in lanes of one wave).
+    __device__ static __forceinline__ uint64_t odd_rows(const uint4 (&r)[kPer], int first_row)   // first_row: of lane 0
+    {
+        uint64_t rows = 0;
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const uint64_t votes = __ballot(odd(r[u]));
+            if (votes == 0) continue;
+#pragma unroll
+            for (int k = 0; k < 64 / kPieces; ++k)
+                if ((votes >> (k * kPieces)) & (~0ull >> (64 - kPieces))) rows |= 1ull << (first_row + k + u * kRowStep);
+        }
+        return rows;
+    }
+
+    // Bytes of one 16-byte piece in the LDS, decoded; `zero`: none of it is to be seen.
+    __device__ static __forceinline__ void put(unsigned char *to, uint4 v, bool zero)
+    {
+        if (zero) v = make_uint4(0, 0, 0, 0);
+        uint4 *w = reinterpret_cast<uint4 *>(to);
+        if constexpr (FORM == kPagesPlain) {
+            w[0] = v;
+        } else {
+            float x[16];
+            Cached<T, FORM>::unpack(v, x);
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    w[e / 4] = make_uint4(__float_as_uint(x[e]), __float_as_uint(x[e + 1]), __float_as_uint(x[e + 2]), __float_as_uint(x[e + 3]));
+            } else {   // (codes are exact in bf16)
+#pragma unroll
+                for (int e = 0; e < 16; e += 8)
+                    w[e / 8] = make_uint4(pack_bf16(x[e], x[e + 1]), pack_bf16(x[e + 2], x[e + 3]),
+                                          pack_bf16(x[e + 4], x[e + 5]), pack_bf16(x[e + 6], x[e + 7]));
+            }
+        }
+    }
+};
+
+// Query rows as operands: rows row_of() of a lane, zeros past d and where there is no row.
+template <typename T, int STEPS>
+__device__ __forceinline__ void load_query(const T *row, int d, int hh, uint4 (&q)[STEPS])
+{
+    constexpr int PER = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int at = (2 * s + hh) * PER;
+        q[s] = row && at < d ? *reinterpret_cast<const uint4 *>(row + at) : make_uint4(0, 0, 0, 0);
+    }
+}
+
+// O^T += V^T P^T over a block of 32 keys: vt is the block's first row of values in the LDS, p the lane's 16 weights.
+template <int D, int PITCH>
+__device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], uint16_t)
+{
+    const int i = lane & 15, hh = lane >> 5;
+    const unsigned char *at = vt + (4 * hh + (i >> 2)) * PITCH + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        union { uint4 u; bf16x8 v; } w;
+        w.u = make_uint4(pack_bf16(p[8 * s], p[8 * s + 1]), pack_bf16(p[8 * s + 2], p[8 * s + 3]),
+                         pack_bf16(p[8 * s + 4], p[8 * s + 5]), pack_bf16(p[8 * s + 6], p[8 * s + 7]));
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            // two groups of four keys, as acc_row() deals them out
+            typedef __attribute__((address_space(3))) bf16x4 lds4;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + 16 * s * PITCH + 64 * b));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + (16 * s + 8) * PITCH + 64 * b));
+            const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w.v, o[b], 0, 0, 0);
+        }
+    }
+}
+template <int D, int PITCH>
+__device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], float)
+{
+    const unsigned char *at = vt + 4 * (lane >> 5) * PITCH + (lane & 31) * 4;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            const float v = *reinterpret_cast<const float *>(at + acc_row(i, 0) * PITCH + 128 * b);
+            o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[b], 0, 0, 0);
+        }
+}
+
+// One tile of logits (NB blocks of 32 keys) to weights 2^(x - m), with the running maximum m and sum l of the lane's
+// query; o is brought to the new maximum.  ks: the keys' scales times c (8-bit), NB x 32 of them; c: otherwise.
+// vis: keys that exist (bit 32 b + key of the block); limit: the lane sees keys 0 .. limit of the tile; `all`: masks hide nothing.
+template <int FORM, int NB, int DB>
+__device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, float c, bool all, uint64_t vis, int limit, int hh,
+                                             float &m, float &l, f32x16 (&o)[DB], float (&p)[NB][16])
+{
+    if constexpr (FORM != kPagesPlain) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 f = *reinterpret_cast<const float4 *>(ks + 32 * b + 8 * j + 4 * hh);
+                x[b][4 * j] *= f.x; x[b][4 * j + 1] *= f.y; x[b][4 * j + 2] *= f.z; x[b][4 * j + 3] *= f.w;
+            }
+        c = 1.f;
+    }
+    if (!all) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = 32 * b + acc_row(i, hh);
+                if (key > limit || !((vis >> key) & 1)) x[b][i] = -INFINITY;
+            }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
+    top = fmaxf(m, other_half_max(top) * c);   // (c > 0)
+    if (__any(top > m)) {
+        const float fade = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        l *= fade;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] *= fade;
+        m = top;
+    }
+    const float shift = m == -INFINITY ? 0.f : m;   // (nothing seen yet: all weights are 2^-inf)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[b][i] = __builtin_amdgcn_exp2f(fmaf(x[b][i], c, -shift));
+            l += p[b][i];
+        }
+}
+
+// The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
+template <int NB>
+__device__ __forceinline__ void scale_weights(const float *vs, bool all, int limit, int hh, float (&p)[NB][16])
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 f = *reinterpret_cast<const float4 *>(vs + 32 * b + 8 * j + 4 * hh);
+            p[b][4 * j] *= f.x; p[b][4 * j + 1] *= f.y; p[b][4 * j + 2] *= f.z; p[b][4 * j + 3] *= f.w;
+        }
+    if (!all) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (32 * b + acc_row(i, hh) > limit) p[b][i] = 0.f;
+    }
+}
+
+// A value of a cached row.
+template <typename T, int FORM> __device__ __forceinline__ float cached_value(const void *rows, long at)
+{
+    if constexpr (FORM == kPagesFp8) {
+        float o[4];
+        decode4<kPagesFp8>(reinterpret_cast<const uint8_t *>(rows)[at], o);
+        return o[0];
+    } else if constexpr (FORM == kPagesInt8) {
+        return (float)reinterpret_cast<const int8_t *>(rows)[at];
+    } else if constexpr (sizeof(T) == 2) {
+        return bf16_to_f32(reinterpret_cast<const uint16_t *>(rows)[at]);
+    } else {
+        return reinterpret_cast<const float *>(rows)[at];
+    }
+}
+
+// What the rows `odd` of a tile, whose values hold infinities or NaN, add to O^T: in the tile's matrix product they would
+// reach the queries that do not see them too (0 x inf), so they went through it as zeros.  Here each of them is a product
+// of its own, which only the lanes that see it keep.  `at`: number of the pool's row of key `lane`.
+template <typename T, int FORM, int NB, int DB>
+__device__ __forceinline__ void add_odd_rows(const void *Vpages, uint64_t odd, int at, int d, const float (&p)[NB][16], int limit,
+                                               int lane, f32x16 (&o)[DB])
+{
+    const int hh = lane >> 5, l32 = lane & 31;
+    for (; odd; odd &= odd - 1) {
+        const int key = __ffsll((unsigned long long)odd) - 1;
+        const long row = __builtin_amdgcn_readlane(at, key);
+        float w = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w += 32 * b + acc_row(i, hh) == key ? p[b][i] : 0.f;
+        w = other_half_sum(w);
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+            const float v = hh == 0 && 32 * b + l32 < d ? cached_value<T, FORM>(Vpages, row * d + 32 * b + l32) : 0.f;
+            const f32x16 with = __builtin_amdgcn_mfma_f32_32x32x2f32(v, hh == 0 ? w : 0.f, o[b], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] = key <= limit ? with[i] : o[b][i];
+        }
+    }
+}
+
+}  // namespace gkv

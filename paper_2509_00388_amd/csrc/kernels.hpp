@@ -232,4 +232,13 @@ hipError_t launch_late_filter(const void *Ac, const void *Kc, int Hkv, int N, in
                               const int32_t *new_src, const int32_t *n_new, void *cand, int32_t *cand_cnt,
                               int32_t *overflow, hipStream_t st);
 
+// ---- paged cache (cache.hip; attention: attend.hpp) -----------------------------------------
+struct PagedBatch;   // paged.hpp
+// Rows of K and V ([row, head], strides in elements) to the places of their tokens, and back.
+hipError_t launch_cache_write(const PagedBatch &b, int dtype, int form, const void *K, const void *V, long row_stride,
+                              long head_stride, void *Kpages, void *Vpages, float *Kscale, float *Vscale, hipStream_t st);
+hipError_t launch_cache_read(const PagedBatch &b, int dtype, int form, const void *Kpages, const void *Vpages,
+                             const float *Kscale, const float *Vscale, void *K, void *V, long row_stride, long head_stride,
+                             hipStream_t st);
+
 }  // namespace gkv

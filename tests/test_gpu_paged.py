@@ -1,0 +1,309 @@
+"""The paged cache through the C ABI: rows written to pages, read back, attention over them, against their definitions in
+64 bits (GPU)."""
+import math
+
+import pytest
+import torch
+
+from paper_2509_00388_amd import binding as gk
+from tests import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+FORMS = [gk.PAGES_PLAIN, gk.PAGES_FP8, gk.PAGES_INT8]
+TYPES = [gk.BF16, gk.FP32]
+
+
+def say(msg):
+    print(msg, flush=True)
+
+
+def on_gpu(t):
+    """The same values and strides on the GPU."""
+    out = torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device="cuda")
+    out.copy_(t)
+    return out
+
+
+def bits(t):
+    return t.cpu().contiguous().view(torch.uint8)
+
+
+# ---- write and read ---------------------------------------------------------------------------------
+
+def written(b, K, V):
+    """What the pools hold after a write, by the definition."""
+    want = {n: t.clone() for n, t in b.pool.items()}
+    for n, x in (("K", K), ("V", V)):
+        if b.form != gk.PAGES_PLAIN:
+            code, scale = pu.encode(x, b.form)
+        for r, s, pos in b.each_row():
+            cell = b.place(s, pos)
+            if cell is None:
+                continue
+            page, at = cell
+            if b.form == gk.PAGES_PLAIN:
+                want[n][page, :, at] = x[r]
+            else:
+                c = code[r].to(torch.int8) if b.form == gk.PAGES_INT8 else code[r].float().to(torch.float8_e4m3fn)
+                want[n].view(torch.uint8)[page, :, at] = c.view(torch.uint8)
+                want[n + "s"][page, :, at] = scale[r].float()
+    return want
+
+
+def check_write(b, K, V):
+    want = written(b, K, V)
+    args = b.device()
+    gk.graphkv_cache_write(b.p, on_gpu(K), on_gpu(V), *args)
+    names = ["K", "V"] + (["Ks", "Vs"] if b.form != gk.PAGES_PLAIN else [])
+    for n, got in zip(names, args[:2] + args[5:]):
+        assert torch.equal(bits(got), bits(want[n])), f"pool {n}"
+    return args
+
+
+def check_read(b, args, by_head=False):
+    if by_head:
+        K, V = (torch.full((b.H, b.rows, b.d), -7.0, dtype=b.p.torch_dtype, device="cuda").transpose(0, 1) for _ in range(2))
+    else:
+        K, V = (torch.full((b.rows, b.H, b.d), -7.0, dtype=b.p.torch_dtype, device="cuda") for _ in range(2))
+    gk.graphkv_cache_read(b.p, *args, K=K, V=V)
+    pools = [t.cpu() for t in args[:2]]
+    scales = [t.cpu() for t in args[5:]] or [None, None]
+    for got, pool, scale in zip((K.cpu(), V.cpu()), pools, scales):
+        want = torch.full((b.rows, b.H, b.d), -7.0).to(b.p.torch_dtype)
+        for r, s, pos in b.each_row():
+            cell = b.place(s, pos)
+            if cell is None:
+                want[r] = 0
+                continue
+            x = pool.view(torch.uint8)[cell[0], :, cell[1]].view(pool.dtype) if b.form == gk.PAGES_FP8 else pool[cell[0], :, cell[1]]
+            want[r] = x if scale is None else (x.float() * scale[cell[0], :, cell[1]][:, None]).to(b.p.torch_dtype)
+        assert torch.equal(bits(got), bits(want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("d,H,ps,how", [(64, 2, 16, "packed"), (128, 8, 64, "fused"), (80, 3, 1, "by_head"), (16, 5, 128, "packed"),
+                                        (512, 1, 8, "fused"), (256, 7, 32, "by_head")])
+def test_rows_written_and_read_back(dtype, form, d, H, ps, how):
+    say(f"write and read dtype={dtype} form={form} d={d} H={H} ps={ps} {how}")
+    b = pu.Batch([(1, 1), (5, 40), (0, 17), (33, 33), (7, 130)], H=H, d=d, ps=ps, dtype=dtype, form=form, before=2, behind=3,
+                 seed=d + H)
+    K, V = (b.random_rows(H, by_head=how == "by_head", fused=4 if how == "fused" else 0) for _ in range(2))
+    K *= torch.exp(3 * torch.randn(b.rows, H, 1, generator=b.g)).to(K.dtype)
+    args = check_write(b, K, V)
+    check_read(b, args, by_head=how != "packed")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", [gk.PAGES_FP8, gk.PAGES_INT8])
+def test_codes_next_to_borders(dtype, form):
+    """Rows whose largest value is a border of the scale, values in the middle of two codes, the least and the largest
+    magnitudes, zeros of both signs."""
+    say(f"codes next to borders dtype={dtype} form={form}")
+    d, H = 64, 4
+    b = pu.Batch([(64, 64)], H=H, d=d, ps=16, dtype=dtype, form=form, seed=3)
+    K, V = b.random_rows(H), b.random_rows(H)
+    most = 127.0 if form == gk.PAGES_INT8 else 448.0
+    for r in range(64):
+        top = most * 2.0 ** (r % 7 - 3)
+        K[r] = (torch.randint(-256, 257, (H, d), generator=b.g) * 0.5 * 2.0 ** (r % 7 - 3)).clamp(-top, top)   # many exact middles
+        K[r, :, 5] = top
+        V[r, :, 7] = [1.0, 448.0, 449.0, 448.0 * 2.0 ** -20, 450.0, 3e38, 1.75, 2.0 ** -99][r % 8]
+        V[r, :, 8] = V[r, :, 7] / 2
+        V[r, :, 9] = -V[r, :, 7]
+    V[9] = 0.0
+    V[10] = -0.0
+    V[11] = 2.0 ** -101
+    check_write(b, K, V)
+
+
+def test_rows_without_a_place():
+    """Page numbers outside the pool, rows that come before a sequence's first token, lengths beyond the table: not written,
+    read as zeros; nothing else changes."""
+    say("rows without a place")
+    for form in FORMS:
+        b = pu.Batch([(6, 30), (5, 3), (4, 50), (3, 20)], H=3, d=32, ps=8, dtype=gk.BF16, form=form, before=1, behind=1, seed=9)
+        b.table[0, 3] = -1
+        b.table[2, 5] = b.p.n_pages
+        b.table[2, 6] = 2 ** 31 - 1
+        K, V = b.random_rows(3), b.random_rows(3)
+        args = check_write(b, K, V)
+        check_read(b, args)
+        # a length beyond the table is cut to it
+        b.len[3] = 10 ** 9
+        args[3] = b.len.cuda()
+        b.len[3] = b.table.shape[1] * b.ps
+        check_read(b, args)
+        # row numbers that do not ascend, or lie outside the tensors: whatever is read, no row outside a sequence is touched
+        for odd in ([-5, 3, 3, 900, 2], [7, 2, 1, 0, -1], [19, 19, 19, 19, 19]):
+            args[4] = torch.tensor(odd, dtype=torch.int32, device="cuda")
+            gk.graphkv_cache_write(b.p, on_gpu(K), on_gpu(V), *args)
+            gk.graphkv_cache_read(b.p, *args)
+            gk.graphkv_attend(b.p, on_gpu(K), *args)
+        torch.cuda.synchronize()
+
+
+def test_long_offsets():
+    """Places beyond 2^32 bytes of a pool."""
+    say("long offsets")
+    H, d, ps, pages = 8, 128, 64, 40000
+    b = pu.Batch([(40, 40)], H=H, d=d, ps=ps, dtype=gk.BF16, seed=1)
+    b.p.n_pages = pages
+    pool = [torch.zeros(pages, H, ps, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    assert (pages - 1) * H * ps * d * 2 > 2 ** 32   # where the last page begins
+    K, V = b.random_rows(H), b.random_rows(H)
+    Q = b.random_rows(H)
+    b.p.n_q_heads = H
+    outs = []
+    for page in (3, pages - 1):
+        b.table[0, 0] = page
+        args = [*pool, b.table.cuda(), b.len.cuda(), b.start.cuda()]
+        gk.graphkv_cache_write(b.p, on_gpu(K), on_gpu(V), *args)
+        k, v = gk.graphkv_cache_read(b.p, *args)
+        assert torch.equal(bits(k), bits(K)) and torch.equal(bits(v), bits(V))
+        assert torch.equal(bits(pool[0][page, :, :40].transpose(0, 1)), bits(K))
+        outs.append(gk.graphkv_attend(b.p, on_gpu(Q), *args))
+    assert torch.equal(outs[0], outs[1])
+
+
+# ---- attention --------------------------------------------------------------------------------------
+
+def run_attend(b, Q, **kw):
+    args = b.device()
+    out = torch.full((b.rows, b.H * b.G, b.d), -7.0, dtype=b.p.torch_dtype, device="cuda")
+    lse = torch.full((b.rows, b.H * b.G), -7.0, device="cuda")
+    ws = torch.randint(0, 256, (gk.graphkv_attend_workspace_bytes(b.p),), dtype=torch.uint8, device="cuda")
+    gk.graphkv_attend(b.p, on_gpu(Q), *args, out=out, lse=lse, ws=ws, **kw)
+    outside = torch.ones(b.rows, dtype=torch.bool)
+    for r, _, _ in b.each_row():
+        outside[r] = False
+    assert (out.cpu()[outside] == -7).all() and (lse.cpu()[outside] == -7).all()
+    return out, lse
+
+
+SHAPES = [
+    # single tokens, few and many tiles, one and several query heads
+    dict(pairs=[(1, 1)], H=1, G=1, d=128), dict(pairs=[(1, 129), (1, 31), (1, 1), (1, 512)], H=2, G=4, d=128),
+    dict(pairs=[(1, 700), (1, 64)], H=3, G=7, d=64, ps=32), dict(pairs=[(1, 300)] * 5, H=2, G=32, d=80, ps=8),
+    # drafts
+    dict(pairs=[(8, 100), (3, 3), (1, 250)], H=2, G=4, d=128, ps=64), dict(pairs=[(4, 77)], H=1, G=8, d=64, ps=1),
+    # chunks, alone and beside single tokens; blocks that end inside a sequence
+    dict(pairs=[(100, 300)], H=2, G=4, d=128), dict(pairs=[(33, 33)], H=3, G=1, d=64, ps=32),
+    dict(pairs=[(1, 150), (70, 200), (8, 90), (129, 130)], H=2, G=2, d=128, ps=32),
+    dict(pairs=[(19, 260), (0, 50), (50, 50)], H=2, G=7, d=96, ps=128),
+    # other head dimensions
+    dict(pairs=[(1, 200), (40, 140)], H=2, G=2, d=256), dict(pairs=[(3, 120)], H=2, G=2, d=160, ps=64),
+    dict(pairs=[(2, 90), (20, 60)], H=1, G=2, d=512), dict(pairs=[(1, 100), (45, 45)], H=2, G=1, d=16),
+    # a group of more query heads than the kernel for few rows takes
+    dict(pairs=[(1, 140)], H=1, G=48, d=64),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_attention(dtype, form, shape):
+    say(f"attention dtype={dtype} form={form} {SHAPES[shape]}")
+    b = pu.Batch(dtype=dtype, form=form, before=1, behind=2, seed=shape, **SHAPES[shape])
+    Q = b.random_rows(b.H * b.G, fused=2 * b.H)
+    out, lse = run_attend(b, Q)
+    pu.check_attend(b, Q, out, lse)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_attention_scalar_kernel(dtype, form):
+    say(f"attention, scalar kernel dtype={dtype} form={form}")
+    b = pu.Batch([(1, 400), (30, 300), (4, 2)], H=2, G=2, d=72 if form == gk.PAGES_PLAIN else 80, ps=16, dtype=dtype, form=form,
+                 impl=gk.IMPL_GENERIC, before=1, behind=1)
+    assert gk.graphkv_attend_workspace_bytes(b.p) == 0
+    Q = b.random_rows(4)
+    out, lse = run_attend(b, Q)
+    pu.check_attend(b, Q, out, lse)
+
+
+@pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_of_rows_that_see_nothing(dtype, impl):
+    """Sequences without tokens, more rows than tokens, pages that are none: zeros and -infinity."""
+    say(f"rows that see nothing dtype={dtype} impl={impl}")
+    b = pu.Batch([(1, 0), (5, 2), (60, 20), (1, 40), (40, 90), (2, 33)], H=2, G=2, d=64, ps=8, dtype=dtype, impl=impl, before=1, behind=1)
+    b.table[3, :] = -1
+    b.table[4, 0] = b.p.n_pages
+    b.table[4, 5] = -2 ** 31
+    b.table[5, 3] = 10 ** 6
+    Q = b.random_rows(4)
+    out, lse = run_attend(b, Q)
+    pu.check_attend(b, Q, out, lse)
+    assert (out.cpu()[1] == 0).all() and (lse.cpu()[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_does_not_see_what_is_hidden(dtype, form, impl, d):
+    """Infinities and NaN in the rest of a page, in other pages and at later positions change nothing, bit for bit."""
+    say(f"hidden places dtype={dtype} form={form} impl={impl} d={d}")
+    b = pu.Batch([(1, 70), (6, 50), (40, 170), (3, 1)], H=2, G=2, d=d, ps=32, dtype=dtype, form=form, impl=impl)
+    Q = b.random_rows(4)
+    clean, clean_lse = run_attend(b, Q)
+    pu.check_attend(b, Q, clean, clean_lse)
+    used = torch.zeros(b.p.n_pages, b.ps, dtype=torch.bool)
+    for s, (_, n) in enumerate(b.pairs):
+        for j in range(n):
+            page, at = b.place(s, j)
+            used[page, at] = True
+    for n in "KV":
+        if form == gk.PAGES_PLAIN:
+            b.pool[n].transpose(1, 2)[~used] = math.nan
+            b.pool[n].transpose(1, 2)[tuple((~used).nonzero()[::3].T)] = math.inf
+        else:
+            b.pool[n].view(torch.uint8).transpose(1, 2)[~used] = 0x7f
+            b.pool[n + "s"].transpose(1, 2)[~used] = math.nan
+    out, lse = run_attend(b, Q)
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+    # a later position: only the rows from it on change
+    for s, late in ((1, 47), (2, 140), (2, 165)):
+        page, at = b.place(s, late)
+        if form == gk.PAGES_PLAIN:
+            b.pool["V"][page, :, at, 5] = math.inf
+            b.pool["K"][page, :, at, 3] = math.nan
+        elif form == gk.PAGES_FP8:
+            b.pool["V"].view(torch.uint8)[page, :, at, 5] = 0x7f
+            b.pool["Ks"][page, :, at] = math.nan
+        else:
+            b.pool["Vs"][page, :, at] = math.inf
+            b.pool["Ks"][page, :, at] = math.nan
+    out, lse = run_attend(b, Q)
+    first_bad = {1: 47, 2: 140}
+    for r, s, pos in b.each_row():
+        if pos < first_bad.get(s, 10 ** 9):
+            assert torch.equal(out[r], clean[r]) and torch.equal(lse[r], clean_lse[r]), (r, s, pos)
+        else:
+            assert torch.isnan(lse[r]).all() and torch.isnan(out[r]).any(), (r, s, pos)
+
+
+def test_attention_with_large_logits_and_a_scale():
+    """Logits of thousands, where only a few weights are left, and a scale of the caller's."""
+    say("large logits")
+    for dtype in TYPES:
+        b = pu.Batch([(1, 200), (50, 190)], H=2, G=2, d=128, dtype=dtype)
+        b.p.softmax_scale = 0.75
+        Q = b.random_rows(4) * 8
+        out, lse = run_attend(b, Q)
+        pu.check_attend(b, Q, out, lse, scale=0.75)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_of_many_sequences(dtype):
+    """More sequences than a workgroup has threads, most of them short, some without new rows."""
+    say(f"many sequences dtype={dtype}")
+    g = torch.Generator().manual_seed(11)
+    pairs = [(int(torch.randint(0, 3, (1,), generator=g)), int(torch.randint(2, 40, (1,), generator=g))) for _ in range(300)]
+    pairs[290] = (40, 60)
+    b = pu.Batch(pairs, H=1, G=2, d=64, ps=8, dtype=dtype, before=1, behind=1)
+    Q = b.random_rows(2)
+    out, lse = run_attend(b, Q)
+    pu.check_attend(b, Q, out, lse)
