@@ -366,7 +366,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return false;
     A = AttendPlan{};
     A.G = p->n_q_heads / p->n_kv_heads;
-    A.generic = p->impl == GRAPHKV_IMPL_GENERIC || !attend_mfma_applies(p->head_dim);
+    A.generic = p->impl == GRAPHKV_IMPL_GENERIC || !attend_mfma_applies(p->dtype, p->head_dim);
     const PagedBatch b = batch_of(p, nullptr, nullptr, nullptr);
     if (A.generic || b.n_rows == 0 || b.n_seqs == 0) return true;
     // (key tiles of all sequences and heads, and the workgroups of the largest launch, are counted in 32 bits)

@@ -25,7 +25,7 @@ __device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1
 
 // ---- how work is cut ----------------------------------------------------------------------------------
 // The lengths are known to the device alone, so each workgroup adds up for itself what lies before its share.  `weight(s)` is
-// the work of sequence s in whatever unit; workgroups of 256 threads, `part`: 10 words of LDS.
+// the work of sequence s in whatever unit; workgroups of 256 threads, `part`: 16 words of LDS.
 template <typename W> __device__ uint32_t weigh(int n_seqs, int of, uint32_t &before, uint32_t *part, W &&weight)
 {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -43,28 +43,39 @@ template <typename W> __device__ uint32_t weigh(int n_seqs, int of, uint32_t &be
     }
     return total;
 }
-// The sequence that holds unit `unit` (below the total), and the units before it.
-template <typename W> __device__ int find_unit(int n_seqs, uint32_t unit, uint32_t &before, uint32_t *part, W &&weight)
+// The sequence that holds unit `first(total)` (below the total), the units before it and the total; -1 if first() says so.
+template <typename W, typename F>
+__device__ int find_share(int n_seqs, uint32_t &total, uint32_t &before, uint32_t *part, W &&weight, F &&first)
 {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    uint32_t base = 0;
-    for (int first = 0; first < n_seqs; first += 256) {
-        const int s = first + tid;
-        const uint32_t w = s < n_seqs ? weight(s) : 0;
-        uint32_t total;
-        __syncthreads();
-        const uint32_t at = base + block_scan_add<4>(w, part, lane, wv, total);
-        if (unit >= at && unit < at + w) { part[8] = (uint32_t)s; part[9] = at; }
-        base += total;
-        __syncthreads();
-        if (unit < base) break;
+    uint32_t w = tid < n_seqs ? weight(tid) : 0;
+    uint32_t at = block_scan_add<4>(w, part, lane, wv, total);
+    if (n_seqs > 256) {   // (more sequences than threads: the total in a pass of its own)
+        uint32_t none;
+        total = weigh(n_seqs, 0, none, part, weight);
     }
-    before = part[9];
-    return __builtin_amdgcn_readfirstlane((int)part[8]);
+    const int64_t unit = first(total);
+    if (unit < 0) return -1;
+    for (int s0 = 0; ; s0 += 256) {
+        if (s0 > 0) {
+            uint32_t here;
+            const uint32_t base = part[12];
+            w = s0 + tid < n_seqs ? weight(s0 + tid) : 0;
+            __syncthreads();
+            at = base + block_scan_add<4>(w, part, lane, wv, here);
+        }
+        if (unit >= at && unit < (int64_t)at + w) { part[10] = (uint32_t)(s0 + tid); part[11] = at; }
+        if (tid == 255) part[12] = at + w;
+        __syncthreads();
+        if (unit < (int64_t)part[12] || s0 + 256 >= n_seqs) break;
+    }
+    before = part[11];
+    return __builtin_amdgcn_readfirstlane((int)part[10]);
 }
 
 // Few rows: the tiles of all (sequence, key-value head) pairs, one after the other, are cut into equal stretches, one a
 // workgroup (no more stretches than tiles).
+constexpr int kMostFewWorkgroups = 512;   // two a compute unit
 struct FewPlan {
     int n_wg, tile_keys, slot_rows, slot_floats;
     float *slots;   // two a workgroup: what its first and its last stretch leave of a pair that others share
@@ -97,7 +108,7 @@ __device__ __forceinline__ uint32_t many_blocks(const SeqRows &q, const AttendAr
 }
 
 // ---- launchers ------------------------------------------------------------------------------------------
-bool attend_mfma_applies(int d);   // whether the matrix-core kernels take this head dimension
+bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
 ManyPlan many_plan(const PagedBatch &b, int G, bool leave_few);
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st);

@@ -28,14 +28,17 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     // Workgroups that follow one another take the heads in turn, so that with eight of them a head's keys and values pass
     // through one XCD's L2; then the blocks of a run of keys, those that see the most keys first.
     const int h = blockIdx.x % b.H, rest = blockIdx.x / b.H, split = rest / pl.blocks;
-    auto weight = [&](int i) { return many_blocks(seq_rows(b, i), a, pl); };
-    uint32_t before;
     // (row numbers that do not ascend can count rows twice: blocks beyond those that the grid and the slots have room for are left out)
-    const uint32_t total = min(weigh(b.n_seqs, 0, before, part, weight), (uint32_t)pl.blocks);
     const uint32_t unit = rest % pl.blocks;
-    if (unit >= total) return;
-    const uint32_t block = total - 1 - unit;
-    const int s = find_unit(b.n_seqs, block, before, part, weight);
+    uint32_t total, before, block = 0;
+    const int s = find_share(b.n_seqs, total, before, part, [&](int i) { return many_blocks(seq_rows(b, i), a, pl); },
+                             [&](uint32_t all) {
+                                 all = min(all, (uint32_t)pl.blocks);
+                                 if (unit >= all) return (int64_t)-1;
+                                 block = all - 1 - unit;
+                                 return (int64_t)block;
+                             });
+    if (s < 0) return;
     const SeqRows sq = seq_rows(b, s);
     const int row0 = (int)(block - before) * kBlockRows, rows = sq.n * a.G;   // stacked rows of the sequence
     const int row = row0 + 32 * wv + l32;
@@ -90,8 +93,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         for (int u = 0; u < L::kPer; ++u) {
             const int r = my_row + u * L::kRowStep, c = my_piece * (16 / L::kCached) * (int)sizeof(T);
             // (places that hold no key of the sequence may hold anything: zeros instead)
-            L::put(kt + r * L::kKeyPitch + c, kr[u], pad || ((hide >> r) & 1));
-            L::put(vt + r * L::kValPitch + c, vr[u], pad || (((hide | odd) >> r) & 1));
+            L::put(kt + r * L::kKeyPitch + c, L::only(kr[u], !(pad || ((hide >> r) & 1))));
+            L::put(vt + r * L::kValPitch + c, L::only(vr[u], !(pad || (((hide | odd) >> r) & 1))));
         }
         if (FORM != kPagesPlain && wv == 0 && lane < KEYS) {
             float *ks = reinterpret_cast<float *>(vt + KEYS * L::kValPitch);
@@ -125,8 +128,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
                 add_block(*reinterpret_cast<const uint4 *>(kt + (32 * n + l32) * L::kKeyPitch + 32 * st + 16 * hh), q[st], x[n], T{});
         }
         float p[NB][16];
-        softmax_tile<FORM, NB, DB>(x, ks, a.c, all, vis, sees - t * KEYS, hh, m, l, o, p);
-        if constexpr (FORM != kPagesPlain) scale_weights<NB>(ks + KEYS, all, sees - t * KEYS, hh, p);
+        const uint64_t seen = seen_keys(vis, sees - t * KEYS, hh);
+        softmax_tile<FORM, NB, DB>(x, ks, a.c, all, seen, hh, m, l, o, p);
+        if constexpr (FORM != kPagesPlain) scale_weights<NB>(ks + KEYS, all, seen, hh, p);
 #pragma unroll
         for (int n = 0; n < NB; ++n) add_values<D, L::kValPitch>(vt + 32 * n * L::kValPitch, p[n], lane, o, T{});
         if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, b.d, p, sees - t * KEYS, lane, o);
@@ -223,7 +227,10 @@ hipError_t go_many(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
 
 template <typename T, int FORM> hipError_t go_many_d(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
 {
-    return a.b.d <= 64 ? go_many<T, FORM, 64>(a, pl, st) : a.b.d <= 128 ? go_many<T, FORM, 128>(a, pl, st) : go_many<T, FORM, 256>(a, pl, st);
+    if (a.b.d <= 64) return go_many<T, FORM, 64>(a, pl, st);
+    if constexpr (sizeof(T) == 2)
+        if (a.b.d > 128) return go_many<T, FORM, 256>(a, pl, st);
+    return go_many<T, FORM, 128>(a, pl, st);
 }
 
 }  // namespace
@@ -256,7 +263,7 @@ hipError_t launch_attend_join_many(const AttendArgs &a, const ManyPlan &pl, int 
     const int D = attend_width(a.b.d);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
     if (dtype == 0)
-        return D == 64 ? go(attend_join_many_kernel<float, 64>) : D == 128 ? go(attend_join_many_kernel<float, 128>) : go(attend_join_many_kernel<float, 256>);
+        return D == 64 ? go(attend_join_many_kernel<float, 64>) : go(attend_join_many_kernel<float, 128>);
     return D == 64 ? go(attend_join_many_kernel<uint16_t, 64>) : D == 128 ? go(attend_join_many_kernel<uint16_t, 128>) : go(attend_join_many_kernel<uint16_t, 256>);
 }
 

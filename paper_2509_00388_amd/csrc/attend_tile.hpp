@@ -50,6 +50,7 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
     static constexpr int kPer = KEYS * kPieces / NT;                             // pieces of a thread
     static constexpr int kRowStep = NT / kPieces;                                // rows between two of its pieces
     static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + 32;
+    static constexpr int kDecoded = 16 / kCached * (int)sizeof(T);               // bytes of a piece in the LDS
     static constexpr int kSteps = D * (int)sizeof(T) / 32;                       // matrix steps of a row of keys
     static_assert(KEYS * kPieces % NT == 0 && NT % kPieces == 0, "whole rows a turn");
 
@@ -77,10 +78,15 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
         return rows;
     }
 
-    // Bytes of one 16-byte piece in the LDS, decoded; `zero`: none of it is to be seen.
-    __device__ static __forceinline__ void put(unsigned char *to, uint4 v, bool zero)
+    // A piece without what is not to be seen.
+    __device__ static __forceinline__ uint4 only(const uint4 &v, bool seen)
     {
-        if (zero) v = make_uint4(0, 0, 0, 0);
+        const uint32_t m = seen ? ~0u : 0u;
+        return make_uint4(v.x & m, v.y & m, v.z & m, v.w & m);
+    }
+    // One piece to its place in the LDS, decoded.
+    __device__ static __forceinline__ void put(unsigned char *to, const uint4 &v)
+    {
         uint4 *w = reinterpret_cast<uint4 *>(to);
         if constexpr (FORM == kPagesPlain) {
             w[0] = v;
@@ -148,11 +154,19 @@ __device__ __forceinline__ void add_values(const unsigned char *vt, const float 
         }
 }
 
+// The keys of a tile that a lane's query sees, those of its half-wave at the places acc_row(i, 0): keys that exist (`vis`) and
+// do not come after the tile's key `limit`.
+__device__ __forceinline__ uint64_t seen_keys(uint64_t vis, int limit, int hh)
+{
+    const uint64_t before = limit < 0 ? 0 : limit >= 63 ? ~0ull : (2ull << limit) - 1;
+    return (vis & before) >> (4 * hh);
+}
+
 // One tile of logits (NB blocks of 32 keys) to weights 2^(x - m), with the running maximum m and sum l of the lane's
 // query; o is brought to the new maximum.  ks: the keys' scales times c (8-bit), NB x 32 of them; c: otherwise.
-// vis: keys that exist (bit 32 b + key of the block); limit: the lane sees keys 0 .. limit of the tile; `all`: masks hide nothing.
+// `all`: every row sees every key; otherwise `seen` has the keys that the lane's query sees (seen_keys()).
 template <int FORM, int NB, int DB>
-__device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, float c, bool all, uint64_t vis, int limit, int hh,
+__device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, float c, bool all, uint64_t seen, int hh,
                                              float &m, float &l, f32x16 (&o)[DB], float (&p)[NB][16])
 {
     if constexpr (FORM != kPagesPlain) {
@@ -169,10 +183,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = 32 * b + acc_row(i, hh);
-                if (key > limit || !((vis >> key) & 1)) x[b][i] = -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i) x[b][i] = (seen >> (32 * b + acc_row(i, 0))) & 1 ? x[b][i] : -INFINITY;
     }
     float top = x[0][0];
 #pragma unroll
@@ -201,7 +212,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
 
 // The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
 template <int NB>
-__device__ __forceinline__ void scale_weights(const float *vs, bool all, int limit, int hh, float (&p)[NB][16])
+__device__ __forceinline__ void scale_weights(const float *vs, bool all, uint64_t seen, int hh, float (&p)[NB][16])
 {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -214,8 +225,7 @@ __device__ __forceinline__ void scale_weights(const float *vs, bool all, int lim
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (32 * b + acc_row(i, hh) > limit) p[b][i] = 0.f;
+            for (int i = 0; i < 16; ++i) p[b][i] = (seen >> (32 * b + acc_row(i, 0))) & 1 ? p[b][i] : 0.f;
     }
 }
 
@@ -258,6 +268,7 @@ __device__ __forceinline__ void add_odd_rows(const void *Vpages, uint64_t odd, i
             const f32x16 with = __builtin_amdgcn_mfma_f32_32x32x2f32(v, hh == 0 ? w : 0.f, o[b], 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] = key <= limit ? with[i] : o[b][i];
+            __builtin_amdgcn_sched_barrier(0);   // (a block at a time: this is rare, the registers are not its own)
         }
     }
 }
