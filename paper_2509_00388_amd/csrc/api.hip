@@ -372,7 +372,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     // (key tiles of all sequences and heads, and the workgroups of the largest launch, are counted in 32 bits)
     const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
     if (((tokens + 127) / 128) * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
-    if (((int64_t)p->n_rows * A.G / kBlockRows + p->n_seqs) * p->n_kv_heads > INT32_MAX) return false;
+    if (((int64_t)p->n_rows * A.G / 64 + p->n_seqs) * p->n_kv_heads > INT32_MAX) return false;
     // Sequences of few rows and of many are different kernels' where both can occur; a batch of one sequence is one or the other.
     A.many = (int64_t)b.max_rows * A.G > kFewRows;
     A.few = !A.many || b.n_seqs > 1;
@@ -382,8 +382,8 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     }
     A.total = A.many_off;
     if (A.many) {
-        A.mp = many_plan(b, A.G, A.few);
-        if (A.mp.splits > 1) A.total += align_up((size_t)A.mp.blocks * A.mp.splits * b.H * A.mp.slot_floats * 4);
+        A.mp = many_plan(b, p->dtype, A.G, A.few);
+        A.total += align_up((size_t)2 * A.mp.n_wg * A.mp.slot_floats * 4);
     }
     return true;
 }
@@ -917,7 +917,7 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
     if (A.many) {
         A.mp.slots = at<float>(ws, A.many_off);
         GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
-        if (A.mp.splits > 1) GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join_many(a, A.mp, p->dtype, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join_many(a, A.mp, p->dtype, st));
     }
     return GRAPHKV_OK;
 }

@@ -49,6 +49,7 @@ __device__ int find_share(int n_seqs, uint32_t &total, uint32_t &before, uint32_
 {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     uint32_t w = tid < n_seqs ? weight(tid) : 0;
+    if (tid == 0) part[10] = (uint32_t)n_seqs;   // (found nowhere: only where row numbers that do not ascend overflow the sums)
     uint32_t at = block_scan_add<4>(w, part, lane, wv, total);
     if (n_seqs > 256) {   // (more sequences than threads: the total in a pass of its own)
         uint32_t none;
@@ -92,25 +93,56 @@ __device__ __forceinline__ int few_owner(uint32_t total, uint32_t tile, int n)
     return (int)((((uint64_t)tile + 1) * n - 1) / total);
 }
 
-// Many rows: a workgroup takes a block of kBlockRows stacked rows of a head and one of `splits` equal runs of the key tiles
-// that the block sees.
-constexpr int kBlockRows = 128;
+// Many rows: blocks of R stacked rows of a head, and of the key tiles that each sees so many units of `step` tiles.  The units of
+// all (sequence, head, block) are cut into equal stretches as above.  A causal chunk's blocks see more and more keys; so that the work
+// before a block follows from the lengths without a sum over blocks, they lie in pairs, the last with the first and so on, whose
+// units are nearly the same number: a pair gets room for W = units(first) + units(last) + 2 of them, what is left of it is
+// empty.  (Units u of a block that sees e keys are max(1, ceil(e / K)); e grows evenly up to rounding down by less than 1, a
+// convex function of evenly spaced numbers is largest in sum at the ends, and rounding up adds less than 1 to either of two.)
+constexpr int kMostManyWorkgroups = 512;   // two a compute unit
 struct ManyPlan {
-    int blocks;       // at least the blocks of all sequences
-    int splits;
+    int n_wg, block_rows, tile_keys, step;
     int leave_few;    // sequences of few rows are the other kernel's
-    int slot_floats;  // (splits > 1) of a (split, block, head): [kBlockRows, D] sums, [kBlockRows] maxima and sums of weights
-    float *slots;
+    int blocks;       // at least the blocks of all sequences
+    int slot_floats;  // [block_rows, D] sums, [block_rows] maxima and sums of weights
+    float *slots;     // two a workgroup
 };
-__device__ __forceinline__ uint32_t many_blocks(const SeqRows &q, const AttendArgs &a, const ManyPlan &p)
+struct ManySeq {
+    int rows, blocks;        // stacked
+    uint32_t pair, middle;   // units of a pair of blocks, of the block that is left in the middle
+    uint32_t per_head;
+};
+// Units of block k of a sequence; `whole`: as if it were full of rows.
+__device__ __forceinline__ uint32_t many_units(const SeqRows &q, int rows, int k, bool whole, const AttendArgs &a, const ManyPlan &p)
 {
-    return p.leave_few && has_few(q, a.G) ? 0 : (uint32_t)((q.n * (long)a.G + kBlockRows - 1) / kBlockRows);
+    const long end = (long)(k + 1) * p.block_rows;
+    const long sees = (long)q.len - q.n + ((whole ? end : min(end, (long)rows)) - 1) / a.G + 1;
+    const long keys = (long)p.tile_keys * p.step;
+    return sees <= keys ? 1u : (uint32_t)((sees + keys - 1) / keys);
+}
+__device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &a, const ManyPlan &p)
+{
+    ManySeq m{};
+    if (q.n <= 0 || (p.leave_few && has_few(q, a.G))) return m;
+    m.rows = q.n * a.G;
+    m.blocks = (m.rows + p.block_rows - 1) / p.block_rows;
+    if (m.blocks > 1) m.pair = many_units(q, m.rows, 0, true, a, p) + many_units(q, m.rows, m.blocks - 1, true, a, p) + 2;
+    if (m.blocks & 1) m.middle = many_units(q, m.rows, m.blocks / 2, false, a, p);
+    m.per_head = m.blocks / 2 * m.pair + m.middle;
+    return m;
+}
+// The first unit of block k, counted from the head's.
+__device__ __forceinline__ uint32_t many_start(const SeqRows &q, const ManySeq &m, int k, const AttendArgs &a, const ManyPlan &p)
+{
+    const int half = m.blocks / 2, mirror = m.blocks - 1 - k;
+    if (k >= half) return (uint32_t)mirror * m.pair;   // the later block of its pair, or the middle one
+    return (uint32_t)k * m.pair + many_units(q, m.rows, mirror, false, a, p);
 }
 
 // ---- launchers ------------------------------------------------------------------------------------------
 bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
-ManyPlan many_plan(const PagedBatch &b, int G, bool leave_few);
+ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_join_few(const AttendArgs &a, const FewPlan &pl, int dtype, hipStream_t st);

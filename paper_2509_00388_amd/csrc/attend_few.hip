@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     const int pieces = b.d * L::kCached / 16, my_piece = lane % L::kPieces, my_row = lane / L::kPieces;
     const int load_piece = min(my_piece, pieces - 1);
 
-    while (tile < last) {
+    while (tile < last && s < b.n_seqs) {
         const SeqRows sq = seq_rows(b, s);
         const uint32_t per_head = few_tiles(sq, a, pl);
         if (per_head == 0 || tile >= before + per_head * b.H) {   // the next sequence
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             wave_sync();
 #pragma unroll
             for (int n = 0; n < NB; ++n) add_values<D, P::kPitch>(kv + 32 * n * P::kPitch, p[n], lane, o, T{});
-            if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, b.d, p, sees - first, lane, o);
+            if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, 0, b.d, p, sees - first, lane, o);
             wave_sync();
             vis = vis1;
             at = at1;
@@ -232,8 +232,8 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, FewP
     const uint32_t total = weigh(b.n_seqs, s, before, part, [&](int i) { return few_tiles(seq_rows(b, i), a, pl) * b.H; });
     const int n_wg = (int)min((uint32_t)pl.n_wg, total);
     const uint32_t first = before + h * per_head, end = first + per_head;
-    const int w0 = few_owner(total, first, n_wg), parts = few_owner(total, end - 1, n_wg) - w0 + 1;
-    if (parts == 1) return;   // finished where it was computed
+    const int w0 = few_owner(total, first, n_wg), parts = min(few_owner(total, end - 1, n_wg), n_wg - 1) - w0 + 1;
+    if (parts <= 1) return;   // finished where it was computed
     // (a workgroup that starts within this pair holds it in its first stretch, one that came from another pair in its last)
     auto slot_of = [&](int w) {
         return pl.slots + (size_t)(2 * w + (few_first(total, w, n_wg) >= first ? 0 : 1)) * pl.slot_floats;

@@ -1,10 +1,13 @@
-// Attention of sequences with many new rows (chunks of a prompt): bound by the matrix cores and the exponentials.
+// Attention of sequences with many new rows (drafts of wide groups, chunks of a prompt): bound by the matrix cores and the
+// exponentials, with few blocks of rows by the read of the keys and values.
 //
-// A workgroup of four waves takes 128 stacked query rows of a head, 32 a wave in operand registers, and streams the keys and
-// values that they see through the LDS in tiles: the next tile's loads are in flight, in registers, while this one is
-// multiplied, and go to the other half of the LDS behind it; one barrier a tile.  Logits stay in registers: each wave turns
-// its 32 x KEYS of them into weights and multiplies them with the values (attend_tile.hpp).  Where the blocks are too few to
-// fill the chip the key tiles of a block are dealt to several workgroups and their parts joined by a second launch.
+// A workgroup of four waves takes a block of 32 RG stacked query rows of a head, 32 of them a wave in operand registers, and
+// streams the keys and values that they see through the LDS in tiles: the next tile's loads are in flight, in registers, while
+// this one is multiplied, and go to the other half of the LDS behind it; one barrier a tile.  With RG = 4 every wave
+// multiplies the whole tile; with RG = 2, for sequences of at most 64 stacked rows, two waves share a group of rows and take half
+// the tile's keys each, and their sums are joined at the end.  Logits stay in registers: each wave turns its 32 x 32 NB of
+// them into weights and multiplies them with the values (attend_tile.hpp).  The work is cut into equal stretches, whatever
+// the lengths (attend.hpp); parts of blocks that several workgroups hold are joined by a second launch.
 #include "attend_tile.hpp"
 #include "kernels.hpp"
 
@@ -12,10 +15,10 @@ namespace gkv {
 
 namespace {
 
-template <typename T, int FORM, int D, int NB>
+template <typename T, int FORM, int D, int NB, int RG>
 __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void attend_many_kernel(AttendArgs a, ManyPlan pl)
 {
-    constexpr int KEYS = 32 * NB, DB = D / 32;
+    constexpr int KS = 4 / RG, KEYS = 32 * NB * KS, DB = D / 32, R = 32 * RG;
     using L = Tile<T, FORM, D, KEYS, 256>;
     constexpr int KEYTILE = KEYS * L::kKeyPitch, HALF = KEYTILE + KEYS * L::kValPitch + (FORM == kPagesPlain ? 0 : 2 * KEYS * 4);
     constexpr uint64_t kAllKeys = KEYS == 64 ? ~0ull : (1ull << KEYS) - 1;
@@ -23,206 +26,298 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     __shared__ uint32_t part[16];
     __shared__ unsigned long long odd_of[3];   // rows of the tile before, of this one and of the next that hold infinities or NaN
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
+    const int group = wv % RG, stream = wv / RG, key0 = 32 * NB * stream;   // the wave's rows of the block, its first key of a tile
     const PagedBatch &b = a.b;
 
-    // Workgroups that follow one another take the heads in turn, so that with eight of them a head's keys and values pass
-    // through one XCD's L2; then the blocks of a run of keys, those that see the most keys first.
-    const int h = blockIdx.x % b.H, rest = blockIdx.x / b.H, split = rest / pl.blocks;
-    // (row numbers that do not ascend can count rows twice: blocks beyond those that the grid and the slots have room for are left out)
-    const uint32_t unit = rest % pl.blocks;
-    uint32_t total, before, block = 0;
-    const int s = find_share(b.n_seqs, total, before, part, [&](int i) { return many_blocks(seq_rows(b, i), a, pl); },
-                             [&](uint32_t all) {
-                                 all = min(all, (uint32_t)pl.blocks);
-                                 if (unit >= all) return (int64_t)-1;
-                                 block = all - 1 - unit;
-                                 return (int64_t)block;
-                             });
+    uint32_t total, before, pos = 0, last = 0;
+    int s = find_share(b.n_seqs, total, before, part, [&](int i) { return many_seq(seq_rows(b, i), a, pl).per_head * b.H; },
+                       [&](uint32_t all) {
+                           const int n = (int)min((uint32_t)pl.n_wg, all), id = blockIdx.x;
+                           if (id >= n) return (int64_t)-1;
+                           // Neighbouring stretches, which read the same keys at about the same time, to one XCD's workgroups.
+                           const int xcd = id % 8, w = xcd * (n / 8) + min(xcd, n % 8) + id / 8;
+                           pos = few_first(all, w, n);
+                           last = few_first(all, w + 1, n);
+                           return (int64_t)pos;
+                       });
     if (s < 0) return;
-    const SeqRows sq = seq_rows(b, s);
-    const int row0 = (int)(block - before) * kBlockRows, rows = sq.n * a.G;   // stacked rows of the sequence
-    const int row = row0 + 32 * wv + l32;
-    const int token = row / a.G, head = h * a.G + row % a.G;
-    const int sees = sq.len - sq.n + token;                                      // last position the lane's row sees
-    const int last_token = min(row0 + kBlockRows, rows) - 1;
-    const int extent = max(0, sq.len - sq.n + last_token / a.G + 1);             // positions the block sees
-    const int first_sees = sq.len - sq.n + row0 / a.G;                           // last position that all its rows see
-    const int tiles = (extent + KEYS - 1) / KEYS;
-    const int t0 = (int)((long)tiles * split / pl.splits), t1 = (int)((long)tiles * (split + 1) / pl.splits);
-
-    const T *qrow = row < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + token) * a.q_row + head * a.q_head : nullptr;
-    uint4 q[L::kSteps];
-    load_query<T>(qrow, b.d, hh, q);
-
-    float m = -INFINITY, l = 0.f;
-    f32x16 o[DB];
-#pragma unroll
-    for (int x = 0; x < DB; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[x][i] = 0.f;
+    const uint32_t mine = pos;
+    const int n_wg = (int)min((uint32_t)pl.n_wg, total);
+    const int slot0 = 2 * ((int)(blockIdx.x % 8) * (n_wg / 8) + min((int)(blockIdx.x % 8), n_wg % 8) + (int)blockIdx.x / 8);
 
     const int pieces = b.d * L::kCached / 16, my_piece = tid % L::kPieces, my_row = tid / L::kPieces;
     const int wave_row = __builtin_amdgcn_readfirstlane(my_row);
     const int load_piece = min(my_piece, pieces - 1);
     const bool pad = my_piece >= pieces;
     const int my_key = lane & (KEYS - 1);   // lane j of each wave looks key j of a tile up
-    auto entry = [&](int t) {
-        const int pos = t * KEYS + my_key;
-        return t < t1 && pos < extent ? page_of(b, s, pos) : -1;
-    };
-    auto place = [&](int page, int t) { return page < 0 ? 0 : pool_row(b, page, h, t * KEYS + my_key); };
-    uint4 kr[L::kPer], vr[L::kPer];
-    float ksr = 0.f, vsr = 0.f;
-    auto load = [&](int at) {
-#pragma unroll
-        for (int u = 0; u < L::kPer; ++u) {
-            const long r = __shfl(at, my_row + u * L::kRowStep, kWave);
-            kr[u] = reinterpret_cast<const uint4 *>(a.Kpages)[r * pieces + load_piece];
-            vr[u] = reinterpret_cast<const uint4 *>(a.Vpages)[r * pieces + load_piece];
-        }
-        if (FORM != kPagesPlain) { ksr = a.Kscale[at]; vsr = a.Vscale[at]; }
-    };
-    auto store = [&](int t, int page, uint64_t vis) {
-        unsigned char *kt = smem + (t & 1) * HALF, *vt = kt + KEYTILE;
-        uint64_t hide = ~vis, odd = 0;
-        if (t * KEYS + KEYS - 1 > first_sees) {   // some rows do not see all of it
-            odd = L::odd_rows(vr, wave_row) & vis;
-            if (odd && lane == 0) atomicOr(&odd_of[t % 3], (unsigned long long)odd);
-        }
-#pragma unroll
-        for (int u = 0; u < L::kPer; ++u) {
-            const int r = my_row + u * L::kRowStep, c = my_piece * (16 / L::kCached) * (int)sizeof(T);
-            // (places that hold no key of the sequence may hold anything: zeros instead)
-            L::put(kt + r * L::kKeyPitch + c, L::only(kr[u], !(pad || ((hide >> r) & 1))));
-            L::put(vt + r * L::kValPitch + c, L::only(vr[u], !(pad || (((hide | odd) >> r) & 1))));
-        }
-        if (FORM != kPagesPlain && wv == 0 && lane < KEYS) {
-            float *ks = reinterpret_cast<float *>(vt + KEYS * L::kValPitch);
-            ks[lane] = page >= 0 ? ksr * a.c : 0.f;
-            ks[KEYS + lane] = page >= 0 ? vsr : 0.f;
-        }
-    };
-    if (tid < 3) odd_of[tid] = 0;
-    int page = entry(t0), at = place(page, t0), page1 = entry(t0 + 1);
-    uint64_t vis = __ballot(page >= 0) & kAllKeys;
-    load(at);
-    __syncthreads();
-    store(t0, page, vis);
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        const int at1 = place(page1, t + 1), page2 = entry(t + 2);
-        const uint64_t vis1 = __ballot(page1 >= 0) & kAllKeys;
-        load(at1);
-        const unsigned char *kt = smem + (t & 1) * HALF, *vt = kt + KEYTILE;
-        const float *ks = reinterpret_cast<const float *>(vt + KEYS * L::kValPitch);
-        const uint64_t odd = odd_of[t % 3];
-        if (tid == 0) odd_of[(t + 2) % 3] = 0;   // (its readers are behind the last barrier, its next writers behind the next)
-        const bool all = vis == kAllKeys && t * KEYS + KEYS - 1 <= first_sees;
-        f32x16 x[NB];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
-#pragma unroll
-            for (int st = 0; st < L::kSteps; ++st)
-                add_block(*reinterpret_cast<const uint4 *>(kt + (32 * n + l32) * L::kKeyPitch + 32 * st + 16 * hh), q[st], x[n], T{});
-        }
-        float p[NB][16];
-        const uint64_t seen = seen_keys(vis, sees - t * KEYS, hh);
-        softmax_tile<FORM, NB, DB>(x, ks, a.c, all, seen, hh, m, l, o, p);
-        if constexpr (FORM != kPagesPlain) scale_weights<NB>(ks + KEYS, all, seen, hh, p);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) add_values<D, L::kValPitch>(vt + 32 * n * L::kValPitch, p[n], lane, o, T{});
-        if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, b.d, p, sees - t * KEYS, lane, o);
-        store(t + 1, page1, vis1);
-        __syncthreads();
-        vis = vis1;
-        at = at1;
-        page1 = page2;
-    }
 
-    l = other_half_sum(l);
-    if (row >= rows) return;
-    if (pl.splits > 1) {
-        float *slot = pl.slots + ((size_t)(split * pl.blocks + block) * b.H + h) * pl.slot_floats;
-        const int r = 32 * wv + l32;
-        if (hh == 0) { slot[kBlockRows * D + 2 * r] = m; slot[kBlockRows * D + 2 * r + 1] = l; }
+    while (pos < last && s < b.n_seqs) {
+        const SeqRows sq = seq_rows(b, s);
+        const ManySeq ms = many_seq(sq, a, pl);
+        if (ms.per_head == 0 || pos >= before + ms.per_head * b.H) {   // the next sequence
+            before += ms.per_head * b.H;
+            ++s;
+            continue;
+        }
+        const int h = (int)((pos - before) / ms.per_head);
+        uint32_t u0 = (pos - before) % ms.per_head;
+        const int pair = ms.pair ? (int)min(u0 / ms.pair, (uint32_t)ms.blocks / 2) : 0;
+        u0 -= (uint32_t)pair * ms.pair;
+        int block = ms.blocks - 1 - pair;
+        uint32_t units = many_units(sq, ms.rows, block, false, a, pl);
+        if (u0 >= units) {
+            u0 -= units;
+            block = pair;
+            units = many_units(sq, ms.rows, block, false, a, pl);
+            if (u0 >= units) {   // the pair's empty rest
+                pos += ms.pair - (ms.pair ? (pos - before) % ms.per_head % ms.pair : 0);
+                continue;
+            }
+        }
+        const uint32_t u1 = min(units, u0 + (last - pos));
+        const int row0 = block * R;                                                  // stacked rows of the sequence
+        const int row = row0 + 32 * group + l32;
+        const int sees = sq.len - sq.n + row / a.G;                                  // last position the lane's row sees
+        const int extent = max(0, sq.len - sq.n + (min(row0 + R, ms.rows) - 1) / a.G + 1);   // positions the block sees
+        const int first_sees = sq.len - sq.n + row0 / a.G;                           // last position that all its rows see
+        const int t0 = (int)u0 * pl.step, t1 = min((int)u1 * pl.step, (extent + KEYS - 1) / KEYS);
+
+        const T *qrow = row < ms.rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / a.G) * a.q_row + (h * a.G + row % a.G) * a.q_head
+                                      : nullptr;
+        uint4 q[L::kSteps];
+        load_query<T>(qrow, b.d, hh, q);
+
+        float m = -INFINITY, l = 0.f;
+        f32x16 o[DB];
 #pragma unroll
         for (int x = 0; x < DB; ++x)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<float4 *>(slot + r * D + 32 * x + 8 * j + 4 * hh) =
-                    make_float4(o[x][4 * j], o[x][4 * j + 1], o[x][4 * j + 2], o[x][4 * j + 3]);
-        return;
-    }
-    if (a.lse && hh == 0) a.lse[(long)(sq.row0 + token) * b.H * a.G + head] = lse_of(m, l);
-    const float f = inverse_of(l);
-    T *to = reinterpret_cast<T *>(a.out) + (sq.row0 + token) * a.o_row + head * a.o_head;
+            for (int i = 0; i < 16; ++i) o[x][i] = 0.f;
+
+        auto entry = [&](int t) {
+            const int at = t * KEYS + my_key;
+            return t < t1 && at < extent ? page_of(b, s, at) : -1;
+        };
+        auto place = [&](int page, int t) { return page < 0 ? 0 : pool_row(b, page, h, t * KEYS + my_key); };
+        uint4 kr[L::kPer], vr[L::kPer];
+        float ksr = 0.f, vsr = 0.f;
+        auto load = [&](int at) {
 #pragma unroll
-    for (int x = 0; x < DB; ++x)
+            for (int u = 0; u < L::kPer; ++u) {
+                const long r = __builtin_amdgcn_ds_bpermute(4 * my_row + 4 * u * L::kRowStep, at);   // of lane my_row + u * kRowStep
+                kr[u] = reinterpret_cast<const uint4 *>(a.Kpages)[r * pieces + load_piece];
+                vr[u] = reinterpret_cast<const uint4 *>(a.Vpages)[r * pieces + load_piece];
+            }
+            if (FORM != kPagesPlain) { ksr = a.Kscale[at]; vsr = a.Vscale[at]; }
+        };
+        auto store = [&](int t, int page, uint64_t vis) {
+            unsigned char *kt = smem + (t & 1) * HALF + my_row * L::kKeyPitch + my_piece * L::kDecoded;
+            unsigned char *vt = smem + (t & 1) * HALF + KEYTILE + my_row * L::kValPitch + my_piece * L::kDecoded;
+            uint64_t odd = 0;
+            if (t * KEYS + KEYS - 1 > first_sees) {   // some rows do not see all of it
+                odd = L::odd_rows(vr, wave_row) & vis;
+                if (odd && lane == 0) atomicOr(&odd_of[t % 3], (unsigned long long)odd);
+            }
+            // (places that hold no key of the sequence may hold anything: zeros instead)
+            const uint64_t kseen = pad ? 0 : vis >> my_row, vseen = pad ? 0 : (vis & ~odd) >> my_row;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = 32 * x + 8 * j + 4 * hh;
-            if (c >= b.d) continue;
-            if constexpr (sizeof(T) == 4)
-                *reinterpret_cast<float4 *>(to + c) = make_float4(o[x][4 * j] * f, o[x][4 * j + 1] * f, o[x][4 * j + 2] * f, o[x][4 * j + 3] * f);
-            else
-                *reinterpret_cast<uint2 *>(to + c) = make_uint2(pack_bf16(o[x][4 * j] * f, o[x][4 * j + 1] * f),
-                                                                pack_bf16(o[x][4 * j + 2] * f, o[x][4 * j + 3] * f));
+            for (int u = 0; u < L::kPer; ++u) {
+                L::put(kt + u * L::kRowStep * L::kKeyPitch, L::only(kr[u], (kseen >> (u * L::kRowStep)) & 1));
+                L::put(vt + u * L::kRowStep * L::kValPitch, L::only(vr[u], (vseen >> (u * L::kRowStep)) & 1));
+            }
+            if (FORM != kPagesPlain && wv == 0 && lane < KEYS) {
+                float *ks = reinterpret_cast<float *>(smem + (t & 1) * HALF + KEYTILE + KEYS * L::kValPitch);
+                ks[lane] = page >= 0 ? ksr * a.c : 0.f;
+                ks[KEYS + lane] = page >= 0 ? vsr : 0.f;
+            }
+        };
+        if (tid < 3) odd_of[tid] = 0;
+        int page = entry(t0), at = place(page, t0), page1 = entry(t0 + 1);
+        uint64_t vis = __ballot(page >= 0) & kAllKeys;
+        load(at);
+        __syncthreads();
+        store(t0, page, vis);
+        __syncthreads();
+        for (int t = t0; t < t1; ++t) {
+            const int at1 = place(page1, t + 1), page2 = entry(t + 2);
+            const uint64_t vis1 = __ballot(page1 >= 0) & kAllKeys;
+            load(at1);
+            const unsigned char *kt = smem + (t & 1) * HALF + key0 * L::kKeyPitch, *vt = smem + (t & 1) * HALF + KEYTILE + key0 * L::kValPitch;
+            const float *ks = reinterpret_cast<const float *>(smem + (t & 1) * HALF + KEYTILE + KEYS * L::kValPitch) + key0;
+            const uint64_t odd = odd_of[t % 3] >> key0 & (~0ull >> (64 - 32 * NB));
+            if (tid == 0) odd_of[(t + 2) % 3] = 0;   // (its readers are behind the last barrier, its next writers behind the next)
+            const bool all = vis == kAllKeys && t * KEYS + KEYS - 1 <= first_sees;
+            f32x16 x[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
+#pragma unroll
+                for (int st = 0; st < L::kSteps; ++st)
+                    add_block(*reinterpret_cast<const uint4 *>(kt + (32 * n + l32) * L::kKeyPitch + 32 * st + 16 * hh), q[st], x[n], T{});
+            }
+            float p[NB][16];
+            const int limit = sees - t * KEYS - key0;
+            const uint64_t seen = seen_keys(vis >> key0, limit, hh);
+            softmax_tile<FORM, NB, DB>(x, ks, a.c, all, seen, hh, m, l, o, p);
+            if constexpr (FORM != kPagesPlain) scale_weights<NB>(ks + KEYS, all, seen, hh, p);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) add_values<D, L::kValPitch>(vt + 32 * n * L::kValPitch, p[n], lane, o, T{});
+            if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, key0, b.d, p, limit, lane, o);
+            store(t + 1, page1, vis1);
+            __syncthreads();
+            vis = vis1;
+            at = at1;
+            page1 = page2;
         }
+
+        l = other_half_sum(l);
+        int G = a.G;
+        asm volatile("" : "+s"(G));   // (what was computed from it before the loop is not kept through it)
+        if constexpr (KS > 1) {
+            // the second stream's sums to the first: [RG][32] maxima and sums, [RG][32][D + 4]
+            float *ml = reinterpret_cast<float *>(smem), *sums = ml + 64 * RG + (group * 32 + l32) * (D + 4) + 4 * hh;
+            if (stream == 1) {
+                if (hh == 0) { ml[2 * (group * 32 + l32)] = m; ml[2 * (group * 32 + l32) + 1] = l; }
+#pragma unroll
+                for (int x = 0; x < DB; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float4 *>(sums + 32 * x + 8 * j) =
+                            make_float4(o[x][4 * j], o[x][4 * j + 1], o[x][4 * j + 2], o[x][4 * j + 3]);
+            }
+            __syncthreads();
+            if (stream == 0) {
+                const float m1 = ml[2 * (group * 32 + l32)], l1 = ml[2 * (group * 32 + l32) + 1], top = fmaxf(m, m1);
+                const float shift = top == -INFINITY ? 0.f : top;
+                const float f = __builtin_amdgcn_exp2f(m - shift), f1 = __builtin_amdgcn_exp2f(m1 - shift);
+                m = top;
+                l = l * f + l1 * f1;
+#pragma unroll
+                for (int x = 0; x < DB; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 y = *reinterpret_cast<const float4 *>(sums + 32 * x + 8 * j);
+                        o[x][4 * j] = o[x][4 * j] * f + y.x * f1;
+                        o[x][4 * j + 1] = o[x][4 * j + 1] * f + y.y * f1;
+                        o[x][4 * j + 2] = o[x][4 * j + 2] * f + y.z * f1;
+                        o[x][4 * j + 3] = o[x][4 * j + 3] * f + y.w * f1;
+                    }
+            }
+            __syncthreads();   // (the next block's tiles come to this place)
+        }
+        const int r = 32 * group + l32;
+        if (stream == 0 && row0 + r < ms.rows) {
+            if (u0 > 0 || u1 < units) {
+                float *slot = pl.slots + (size_t)(slot0 + (pos == mine ? 0 : 1)) * pl.slot_floats;
+                if (hh == 0) { slot[R * D + 2 * r] = m; slot[R * D + 2 * r + 1] = l; }
+#pragma unroll
+                for (int x = 0; x < DB; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float4 *>(slot + r * D + 32 * x + 8 * j + 4 * hh) =
+                            make_float4(o[x][4 * j], o[x][4 * j + 1], o[x][4 * j + 2], o[x][4 * j + 3]);
+            } else {
+                const int token = (row0 + r) / G, head = h * G + (row0 + r) % G;
+                if (a.lse && hh == 0) a.lse[(long)(sq.row0 + token) * b.H * G + head] = lse_of(m, l);
+                const float f = inverse_of(l);
+                T *to = reinterpret_cast<T *>(a.out) + (sq.row0 + token) * a.o_row + head * a.o_head;
+#pragma unroll
+                for (int x = 0; x < DB; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int c = 32 * x + 8 * j + 4 * hh;
+                        if (c >= b.d) continue;
+                        if constexpr (sizeof(T) == 4)
+                            *reinterpret_cast<float4 *>(to + c) = make_float4(o[x][4 * j] * f, o[x][4 * j + 1] * f, o[x][4 * j + 2] * f, o[x][4 * j + 3] * f);
+                        else
+                            *reinterpret_cast<uint2 *>(to + c) = make_uint2(pack_bf16(o[x][4 * j] * f, o[x][4 * j + 1] * f),
+                                                                            pack_bf16(o[x][4 * j + 2] * f, o[x][4 * j + 3] * f));
+                    }
+            }
+        }
+        pos += u1 - u0;
+    }
 }
 
-// The parts of a block's runs of keys: a workgroup a (row, key-value head).
+// The parts of blocks that several workgroups held: a workgroup 32 rows of a (block, head).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, ManyPlan pl)
 {
     __shared__ uint32_t part[16];
+    __shared__ float tops[32], sums[32];
     const PagedBatch &b = a.b;
-    const int row = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
-    const int s = seq_of_row(b, row, tid & 63);
-    if (s >= b.n_seqs) return;
-    const SeqRows sq = seq_rows(b, s);
-    if (row < sq.row0 || row >= sq.row0 + sq.n || many_blocks(sq, a, pl) == 0) return;
+    const int h = blockIdx.x % b.H, tid = threadIdx.x;
+    uint32_t blocks, first_block;
+    const int s = find_share(b.n_seqs, blocks, first_block, part, [&](int i) { return (uint32_t)many_seq(seq_rows(b, i), a, pl).blocks; },
+                             [&](uint32_t all) { return blockIdx.x / b.H < all ? (int64_t)(blockIdx.x / b.H) : (int64_t)-1; });
+    if (s < 0 || s >= b.n_seqs) return;
+    __syncthreads();
     uint32_t before;
-    weigh(b.n_seqs, s, before, part, [&](int i) { return many_blocks(seq_rows(b, i), a, pl); });
-    if (before + ((row - sq.row0 + 1) * a.G - 1) / kBlockRows >= (uint32_t)pl.blocks) return;
-    for (int e = tid; e < a.G * (D / 4); e += 256) {
-        const int g = e / (D / 4), c4 = 4 * (e % (D / 4)), stacked = (row - sq.row0) * a.G + g, r = stacked % kBlockRows;
-        const float *slot = pl.slots + ((size_t)(before + stacked / kBlockRows) * b.H + h) * pl.slot_floats;
-        const size_t step = (size_t)pl.blocks * b.H * pl.slot_floats;
+    const uint32_t total = weigh(b.n_seqs, s, before, part, [&](int i) { return many_seq(seq_rows(b, i), a, pl).per_head * b.H; });
+    const SeqRows sq = seq_rows(b, s);
+    const ManySeq ms = many_seq(sq, a, pl);
+    const int block = (int)(blockIdx.x / b.H - first_block), r0 = 32 * blockIdx.y, rows = min(ms.rows - block * pl.block_rows - r0, 32);
+    if (rows <= 0) return;
+    const int n_wg = (int)min((uint32_t)pl.n_wg, total);
+    const uint32_t first = before + h * ms.per_head + many_start(sq, ms, block, a, pl);
+    const uint32_t end = first + many_units(sq, ms.rows, block, false, a, pl);
+    const int w0 = few_owner(total, first, n_wg), w1 = min(few_owner(total, end - 1, n_wg), n_wg - 1);
+    if (w0 >= w1) return;   // finished where it was computed
+    auto slot_of = [&](int w) { return pl.slots + (size_t)(2 * w + (few_first(total, w, n_wg) >= first ? 0 : 1)) * pl.slot_floats; };
+    const int stat = pl.block_rows * D;
+    if (tid < rows) {
         float top = -INFINITY, sum = 0.f;
-        for (int k = 0; k < pl.splits; ++k) top = fmaxf(top, slot[k * step + kBlockRows * D + 2 * r]);
+        for (int w = w0; w <= w1; ++w) top = fmaxf(top, slot_of(w)[stat + 2 * (r0 + tid)]);
         const float shift = top == -INFINITY ? 0.f : top;
+        for (int w = w0; w <= w1; ++w)
+            sum = fmaf(slot_of(w)[stat + 2 * (r0 + tid) + 1], __builtin_amdgcn_exp2f(slot_of(w)[stat + 2 * (r0 + tid)] - shift), sum);
+        tops[tid] = shift;
+        sums[tid] = inverse_of(sum);
+        const int stacked = block * pl.block_rows + r0 + tid;
+        if (a.lse) a.lse[(long)(sq.row0 + stacked / a.G) * b.H * a.G + h * a.G + stacked % a.G] = lse_of(top, sum);
+    }
+    __syncthreads();
+    for (int e = tid; e < rows * (D / 4); e += 256) {
+        const int r = e / (D / 4), c4 = 4 * (e % (D / 4)), stacked = block * pl.block_rows + r0 + r;
+        if (c4 >= b.d) continue;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < pl.splits; ++k) {
-            const float *p = slot + k * step;
-            const float f = __builtin_amdgcn_exp2f(p[kBlockRows * D + 2 * r] - shift);
-            const float4 y = *reinterpret_cast<const float4 *>(p + r * D + c4);
-            sum = fmaf(p[kBlockRows * D + 2 * r + 1], f, sum);
+        for (int w = w0; w <= w1; ++w) {
+            const float *p = slot_of(w);
+            const float f = __builtin_amdgcn_exp2f(p[stat + 2 * (r0 + r)] - tops[r]);
+            const float4 y = *reinterpret_cast<const float4 *>(p + (r0 + r) * D + c4);
             v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
         }
-        if (a.lse && c4 == 0) a.lse[(long)row * b.H * a.G + h * a.G + g] = lse_of(top, sum);
-        if (c4 >= b.d) continue;
-        const float f = inverse_of(sum);
-        T *to = reinterpret_cast<T *>(a.out) + row * a.o_row + (h * a.G + g) * a.o_head + c4;
+        const float f = sums[r];
+        T *to = reinterpret_cast<T *>(a.out) + (sq.row0 + stacked / a.G) * a.o_row + (h * a.G + stacked % a.G) * a.o_head + c4;
         if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
         else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f));
     }
 }
 
-// 32-key blocks of a tile: two, where the LDS holds two such tiles for two workgroups.
-template <typename T, int D> constexpr int many_key_blocks() { return D * (int)sizeof(T) <= 256 ? 2 : 1; }
+// Keys of a tile: 64, where the LDS holds two such tiles for two workgroups, otherwise 32.
+template <typename T, int D> constexpr int many_tile_keys() { return D * (int)sizeof(T) <= 256 ? 64 : 32; }
+
+template <typename T, int FORM, int D, int RG>
+hipError_t go_many_rows(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
+{
+    constexpr int KEYS = many_tile_keys<T, D>(), NB = KEYS * RG / 128;
+    using L = Tile<T, FORM, D, KEYS, 256>;
+    const int tiles = 2 * (KEYS * (L::kKeyPitch + L::kValPitch) + (FORM == kPagesPlain ? 0 : 8 * KEYS));
+    const int joined = RG == 4 ? 0 : (64 * RG + 32 * RG * (D + 4)) * 4;
+    const int lds = tiles > joined ? tiles : joined;
+    auto kernel = attend_many_kernel<T, FORM, D, NB, RG>;
+    if (lds > 64 * 1024 && !allow_big_lds(reinterpret_cast<const void *>(kernel))) return hipErrorInvalidValue;
+    kernel<<<pl.n_wg, 256, lds, st>>>(a, pl);
+    return hipGetLastError();
+}
 
 template <typename T, int FORM, int D>
 hipError_t go_many(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
 {
-    constexpr int NB = many_key_blocks<T, D>(), KEYS = 32 * NB;
-    using L = Tile<T, FORM, D, KEYS, 256>;
-    const int lds = 2 * (KEYS * (L::kKeyPitch + L::kValPitch) + (FORM == kPagesPlain ? 0 : 8 * KEYS));
-    auto kernel = attend_many_kernel<T, FORM, D, NB>;
-    if (lds > 64 * 1024 && !allow_big_lds(reinterpret_cast<const void *>(kernel))) return hipErrorInvalidValue;
-    kernel<<<dim3((unsigned)((size_t)pl.blocks * pl.splits * a.b.H)), 256, lds, st>>>(a, pl);
-    return hipGetLastError();
+    if constexpr (many_tile_keys<T, D>() == 64)
+        if (pl.block_rows == 64) return go_many_rows<T, FORM, D, 2>(a, pl, st);
+    return go_many_rows<T, FORM, D, 4>(a, pl, st);
 }
 
 template <typename T, int FORM> hipError_t go_many_d(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
@@ -235,16 +330,23 @@ template <typename T, int FORM> hipError_t go_many_d(const AttendArgs &a, const 
 
 }  // namespace
 
-ManyPlan many_plan(const PagedBatch &b, int G, bool leave_few)
+ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
 {
     const int D = attend_width(b.d);
     ManyPlan p{};
     p.leave_few = leave_few;
-    p.blocks = (int)((long)b.n_rows * G / kBlockRows) + b.n_seqs;
-    // Two workgroups a compute unit, but runs of at least 512 keys.
-    const long cap = (((long)b.table_pages << b.page_shift) + 511) / 512, want = 512 / ((long)p.blocks * b.H);
-    p.splits = (int)(want < 1 ? 1 : want < cap ? want : cap);
-    p.slot_floats = kBlockRows * (D + 2);
+    p.tile_keys = D * (dtype == 0 ? 4 : 2) <= 256 ? 64 : 32;
+    p.block_rows = p.tile_keys == 64 && (long)b.max_rows * G <= 64 ? 64 : 128;
+    p.blocks = (int)((long)b.n_rows * G / p.block_rows) + b.n_seqs;
+    p.slot_floats = p.block_rows * (D + 2);
+    // Units of 256 keys, or more where their number could pass 31 bits.
+    const long cap = (long)b.table_pages << b.page_shift;
+    long units = 0;
+    for (p.step = 256 / p.tile_keys;; p.step *= 2) {
+        units = ((long)p.blocks / 2 + b.n_seqs) * (2 * (cap / ((long)p.tile_keys * p.step) + 1) + 2) * b.H;
+        if (units <= INT32_MAX) break;
+    }
+    p.n_wg = units < kMostManyWorkgroups ? (int)units : kMostManyWorkgroups;
     return p;
 }
 
@@ -259,7 +361,7 @@ hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype
 
 hipError_t launch_attend_join_many(const AttendArgs &a, const ManyPlan &pl, int dtype, hipStream_t st)
 {
-    const dim3 grid(a.b.n_rows, a.b.H);
+    const dim3 grid(pl.blocks * a.b.H, pl.block_rows / 32);
     const int D = attend_width(a.b.d);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
     if (dtype == 0)

@@ -247,15 +247,15 @@ template <typename T, int FORM> __device__ __forceinline__ float cached_value(co
 
 // What the rows `odd` of a tile, whose values hold infinities or NaN, add to O^T: in the tile's matrix product they would
 // reach the queries that do not see them too (0 x inf), so they went through it as zeros.  Here each of them is a product
-// of its own, which only the lanes that see it keep.  `at`: number of the pool's row of key `lane`.
+// of its own, which only the lanes that see it keep.  Lane key0 + j has in `at` the number of the pool's row of key j.
 template <typename T, int FORM, int NB, int DB>
-__device__ __forceinline__ void add_odd_rows(const void *Vpages, uint64_t odd, int at, int d, const float (&p)[NB][16], int limit,
+__device__ __forceinline__ void add_odd_rows(const void *Vpages, uint64_t odd, int at, int key0, int d, const float (&p)[NB][16], int limit,
                                                int lane, f32x16 (&o)[DB])
 {
     const int hh = lane >> 5, l32 = lane & 31;
     for (; odd; odd &= odd - 1) {
         const int key = __ffsll((unsigned long long)odd) - 1;
-        const long row = __builtin_amdgcn_readlane(at, key);
+        const long row = __builtin_amdgcn_readlane(at, key0 + key);
         float w = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
