@@ -126,7 +126,7 @@ class PagedParams:
 
     @property
     def page_dtype(self):
-        return {PAGES_FP8: torch.float8_e4m3fn, PAGES_INT8: torch.int8}.get(self.page_format, self.torch_dtype)
+        return torch.float8_e4m3fn if self.page_format == PAGES_FP8 else torch.int8 if self.page_format == PAGES_INT8 else self.torch_dtype
 
 
 _lib = None
@@ -400,52 +400,68 @@ def graphkv_compress_batched(p: Params, n_layers: int, budgets, Kc, Vc, Qw, Kout
 
 
 # ---- paged cache ----
+# (These calls sit between the kernels of a decoding step, a few microseconds each, so their checks are kept short.)
+
+def _paged_arg(t, name: str, dtype, numel: int, dev):
+    """_arg() for a tensor on a device that is known already."""
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    _arg(t, name, dtype, numel)
+    raise GraphKVError(f"{name} must be on {dev}, where the pools are")
+
 
 def _rows_arg(p: PagedParams, t, name: str, heads: int, dev):
     """(address, strides) of a tensor [n_rows, heads, d], any strides that keep a row's d values together."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != dev:
-        raise GraphKVError(f"{name} must be a tensor on the pools' device")
+    d = p.head_dim
+    if not isinstance(t, torch.Tensor) or t.device != dev:
+        raise GraphKVError(f"{name} must be a tensor on {dev}, where the pools are")
     if t.dtype != p.torch_dtype:
         raise GraphKVError(f"{name} must have dtype {p.torch_dtype}, got {t.dtype}")
-    if t.shape != (p.n_rows, heads, p.head_dim):
-        raise GraphKVError(f"{name} must have shape {(p.n_rows, heads, p.head_dim)}, got {tuple(t.shape)}")
+    if t.shape != (p.n_rows, heads, d):
+        raise GraphKVError(f"{name} must have shape {(p.n_rows, heads, d)}, got {tuple(t.shape)}")
+    if p.n_rows == 0:
+        return t.data_ptr(), (0, 0)
     row, head, one = t.stride()
     # (the stride of a dimension of one entry is never used; it is told as what a packed tensor has)
     if heads == 1:
-        head = p.head_dim
-    if p.n_rows <= 1:
+        head = d
+    if p.n_rows == 1:
         row = heads * head
-    unit = 16 // t.element_size()
-    if t.numel() and (one != 1 or row < p.head_dim or head < p.head_dim or row % unit or head % unit):
-        raise GraphKVError(f"{name}: rows of {p.head_dim} values together, strides in multiples of 16 bytes; got strides {t.stride()}")
-    return t.data_ptr(), (row, head) if t.numel() else (0, 0)
+    unit = 4 if p.dtype == FP32 else 8
+    if (one != 1 and d > 1) or row < d or head < d or row % unit or head % unit:
+        raise GraphKVError(f"{name}: rows of {d} values together, strides in multiples of 16 bytes; got strides {t.stride()}")
+    return t.data_ptr(), (row, head)
 
 
 def _pool_args(p: PagedParams, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale):
     """Addresses of what the calls on a paged cache share, checked; the device they live on."""
-    rows = p.n_pages * p.n_kv_heads * p.page_tokens
-    coded = p.page_format != PAGES_PLAIN
-    told = ((Kpages, "Kpages", p.page_dtype, rows * p.head_dim), (Vpages, "Vpages", p.page_dtype, rows * p.head_dim),
-            (Kscale if coded else None, "Kscale", torch.float32, rows), (Vscale if coded else None, "Vscale", torch.float32, rows),
-            (table, "table", torch.int32, p.n_seqs * p.table_pages), (seq_len, "seq_len", torch.int32, p.n_seqs),
-            (row_start, "row_start", torch.int32, p.n_seqs + 1))
-    at = [_arg(t, name, dtype, n, optional=not coded and name in ("Kscale", "Vscale")) for t, name, dtype, n in told]
-    dev = Kpages.device
-    if any(t is not None and t.device != dev for t, *_ in told):
-        raise GraphKVError("the pools, scales, table, seq_len and row_start must be on one device")
-    return at, dev
+    if not isinstance(Kpages, torch.Tensor) or not Kpages.is_cuda:
+        raise GraphKVError("Kpages must be a contiguous device tensor")
+    dev, rows, dtype = Kpages.device, p.n_pages * p.n_kv_heads * p.page_tokens, p.page_dtype
+    ks = vs = None
+    if p.page_format != PAGES_PLAIN:
+        ks = _paged_arg(Kscale, "Kscale", torch.float32, rows, dev)
+        vs = _paged_arg(Vscale, "Vscale", torch.float32, rows, dev)
+    return (_paged_arg(Kpages, "Kpages", dtype, rows * p.head_dim, dev), _paged_arg(Vpages, "Vpages", dtype, rows * p.head_dim, dev),
+            ks, vs, _paged_arg(table, "table", torch.int32, p.n_seqs * p.table_pages, dev),
+            _paged_arg(seq_len, "seq_len", torch.int32, p.n_seqs, dev),
+            _paged_arg(row_start, "row_start", torch.int32, p.n_seqs + 1, dev)), dev
 
 
 def _new_rows(p: PagedParams, heads: int, dev):
     return torch.empty((p.n_rows, heads, p.head_dim), dtype=p.torch_dtype, device=dev)
 
 
+# (torch.cuda.current_stream() builds an object for it: 2.8 us where this takes 0.1)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call_on(dev, f, *args):
-    """Calls f(*args, stream) with the tensors' device as the current one, on its current stream."""
-    if dev.index is None or dev.index == torch.cuda.current_device():
-        return f(*args, _stream())
+    """Calls f(*args, stream) with the tensors' device as the current one, on that device's current stream."""
+    if dev.index == torch.cuda.current_device():
+        return f(*args, _raw_stream(dev.index))
     with torch.cuda.device(dev):
-        return f(*args, _stream())
+        return f(*args, _raw_stream(dev.index))
 
 
 def graphkv_cache_write(p: PagedParams, K, V, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None):
@@ -489,13 +505,11 @@ def graphkv_attend(p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start,
     qp, qs = _rows_arg(p, Q, "Q", p.n_q_heads, dev)
     out = _new_rows(p, p.n_q_heads, dev) if out is None else out
     op, os_ = _rows_arg(p, out, "out", p.n_q_heads, dev)
-    lp = _arg(lse, "lse", torch.float32, p.n_rows * p.n_q_heads, optional=True)
+    lp = None if lse is None else _paged_arg(lse, "lse", torch.float32, p.n_rows * p.n_q_heads, dev)
     cp = p.c(qs, os_)
     if ws is None:
         ws = torch.empty(load_library().graphkv_attend_workspace_bytes(ctypes.byref(cp)), dtype=torch.uint8, device=dev)
-    wp = _arg(ws, "ws", torch.uint8, 0)
-    if ws.device != dev or (lse is not None and lse.device != dev):
-        raise GraphKVError("lse and ws must be on the pools' device")
+    wp = _paged_arg(ws, "ws", torch.uint8, 0, dev)
     _check(_call_on(dev, load_library().graphkv_attend, ctypes.byref(cp), qp, *at, op, lp, wp, ws.numel()))
     return out
 

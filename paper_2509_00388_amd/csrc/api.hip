@@ -356,7 +356,7 @@ struct AttendPlan {
     bool generic, few, many;
     FewPlan fp;
     ManyPlan mp;
-    size_t many_off, total;
+    size_t few_slots, many_records, many_slots, total;   // places in the workspace
 };
 
 bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
@@ -378,12 +378,14 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     A.few = !A.many || b.n_seqs > 1;
     if (A.few) {
         A.fp = few_plan(b, p->dtype, p->page_format, A.G);
-        A.many_off = align_up((size_t)2 * A.fp.n_wg * A.fp.slot_floats * 4);
+        A.few_slots = align_up(join_record_bytes(A.fp.join));
+        A.total = A.few_slots + align_up(join_slot_bytes(A.fp.join));
     }
-    A.total = A.many_off;
     if (A.many) {
         A.mp = many_plan(b, p->dtype, A.G, A.few);
-        A.total += align_up((size_t)2 * A.mp.n_wg * A.mp.slot_floats * 4);
+        A.many_records = A.total;
+        A.many_slots = A.many_records + align_up(join_record_bytes(A.mp.join));
+        A.total = A.many_slots + align_up(join_slot_bytes(A.mp.join));
     }
     return true;
 }
@@ -910,14 +912,16 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
         return GRAPHKV_OK;
     }
     if (A.few) {
-        A.fp.slots = at<float>(ws, 0);
+        A.fp.join.records = at<JoinRecord>(ws, 0);
+        A.fp.join.slots = at<float>(ws, A.few_slots);
         GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, st));
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join_few(a, A.fp, p->dtype, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, p->dtype, st));
     }
     if (A.many) {
-        A.mp.slots = at<float>(ws, A.many_off);
+        A.mp.join.records = at<JoinRecord>(ws, A.many_records);
+        A.mp.join.slots = at<float>(ws, A.many_slots);
         GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join_many(a, A.mp, p->dtype, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.mp.join, p->dtype, st));
     }
     return GRAPHKV_OK;
 }

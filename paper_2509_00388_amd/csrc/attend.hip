@@ -75,7 +75,82 @@ __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
     if (a.lse && tid == 0) a.lse[(long)row * a.b.H * a.G + hq] = lse_of(m, l);
 }
 
+// The parts of blocks of rows that several workgroups hold, put together: workgroup (w, y) takes rows y * rows_per_wg and on of the
+// block whose first part workgroup w held.  A row is 256 / GROUPS lanes wide, four sums a lane; where the parts are many, several
+// groups of lanes share a row's.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan pl)
+{
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ float4 sums[GROUPS][LANES];
+    __shared__ float totals[GROUPS];
+    const JoinRecord rec = pl.records[blockIdx.x];
+    const int first = blockIdx.y * pl.rows_per_wg, last = min(first + pl.rows_per_wg, rec.rows);
+    if (rec.parts == 0 || first >= last) return;
+    int share = 1;   // groups a row
+    while (share < GROUPS && (share < rec.parts / 4 || 2 * share * (last - first) <= GROUPS)) share *= 2;
+    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, mine = group % share, at_once = GROUPS / share;
+    const float *slot0 = pl.slots + (size_t)rec.slot * pl.slot_floats;
+    const float *slots = pl.slots + (size_t)2 * blockIdx.x * pl.slot_floats;   // part k > 0: 2 k slots further
+    for (int r0 = first; r0 < last; r0 += at_once) {
+        const int r = min(r0 + group / share, last - 1);
+        const int stat = pl.slot_rows * D + 2 * r, at = r * D + 4 * lane;
+        float m = -INFINITY, l = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int k = mine; k < rec.parts; k += share) {
+            const float *p = k == 0 ? slot0 : slots + (size_t)2 * k * pl.slot_floats;
+            const float4 y = *reinterpret_cast<const float4 *>(p + at);
+            const float2 ml = *reinterpret_cast<const float2 *>(p + stat);
+            const float top = fmaxf(m, ml.x), shift = top == -INFINITY ? 0.f : top;
+            const float f = __builtin_amdgcn_exp2f(m - shift), g = __builtin_amdgcn_exp2f(ml.x - shift);
+            m = top;
+            l = l * f + ml.y * g;
+            v.x = v.x * f + y.x * g; v.y = v.y * f + y.y * g; v.z = v.z * f + y.z * g; v.w = v.w * f + y.w * g;
+        }
+        if (share > 1) {
+            // (groups of a row: bring them to the row's maximum, then one of them adds them up)
+            __syncthreads();
+            if (lane == 0) totals[group] = m;
+            __syncthreads();
+            const int g0 = group - mine;
+            float top = -INFINITY;
+            for (int g = 0; g < share; ++g) top = fmaxf(top, totals[g0 + g]);
+            const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+            m = top;
+            sums[group][lane] = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+            __syncthreads();
+            if (lane == 0) totals[group] = l * f;
+            __syncthreads();
+            l = 0.f;
+            v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int g = 0; g < share; ++g) {
+                const float4 y = sums[g0 + g][lane];
+                l += totals[g0 + g];
+                v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+            }
+        }
+        if (mine != 0 || r0 + group / share >= last) continue;
+        const int stacked = rec.stacked + r, token = rec.row0 + stacked / a.G, head = rec.h * a.G + stacked % a.G;
+        if (a.lse && lane == 0) a.lse[(long)token * a.b.H * a.G + head] = lse_of(m, l);
+        if (4 * lane >= a.b.d) continue;
+        const float f = inverse_of(l);
+        T *to = reinterpret_cast<T *>(a.out) + token * a.o_row + head * a.o_head + 4 * lane;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f));
+    }
+}
+
 }  // namespace
+
+hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &pl, int dtype, hipStream_t st)
+{
+    const dim3 grid(pl.n_wg, (pl.slot_rows + pl.rows_per_wg - 1) / pl.rows_per_wg);
+    const int D = attend_width(a.b.d);
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
+    if (dtype == 0) return D == 64 ? go(attend_join_kernel<float, 64>) : go(attend_join_kernel<float, 128>);
+    return D == 64 ? go(attend_join_kernel<uint16_t, 64>) : D == 128 ? go(attend_join_kernel<uint16_t, 128>) : go(attend_join_kernel<uint16_t, 256>);
+}
 
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st)
 {

@@ -74,23 +74,41 @@ __device__ int find_share(int n_seqs, uint32_t &total, uint32_t &before, uint32_
     return __builtin_amdgcn_readfirstlane((int)part[10]);
 }
 
+// Equal stretches of `total` units for n workgroups: the first unit of the w-th, and the one that takes a unit.
+__device__ __forceinline__ uint32_t stretch_first(uint32_t total, int w, int n) { return (uint32_t)((uint64_t)total * w / n); }
+__device__ __forceinline__ int stretch_owner(uint32_t total, uint32_t unit, int n)
+{
+    return min((int)((((uint64_t)unit + 1) * n - 1) / total), n - 1);
+}
+
+// What a workgroup leaves of a block of rows that others hold parts of too: every workgroup has two slots, for the part its
+// stretch begins with and the part it ends with, and a record of a block whose first part it holds.  The other parts of
+// that block are the first slots of the workgroups behind it.
+struct JoinRecord {
+    int32_t parts;       // 0: none
+    int32_t slot;        // of the first part
+    int32_t row0, h;     // the sequence's first row, the key-value head
+    int32_t stacked, rows;   // stacked rows stacked .. stacked + rows - 1 of the sequence
+    int32_t unused[2];
+};
+struct JoinPlan {
+    int n_wg, slot_rows, slot_floats;   // a slot: [slot_rows, D] sums, [slot_rows] maxima and sums of weights
+    int rows_per_wg;
+    JoinRecord *records;   // [n_wg]
+    float *slots;          // [2 n_wg, slot_floats]
+};
+
 // Few rows: the tiles of all (sequence, key-value head) pairs, one after the other, are cut into equal stretches, one a
 // workgroup (no more stretches than tiles).
 constexpr int kMostFewWorkgroups = 512;   // two a compute unit
 struct FewPlan {
-    int n_wg, tile_keys, slot_rows, slot_floats;
-    float *slots;   // two a workgroup: what its first and its last stretch leave of a pair that others share
+    JoinPlan join;
+    int tile_keys;
 };
 __device__ __forceinline__ bool has_few(const SeqRows &q, int G) { return q.n > 0 && q.n * (long)G <= kFewRows; }
 __device__ __forceinline__ uint32_t few_tiles(const SeqRows &q, const AttendArgs &a, const FewPlan &p)   // of a head
 {
     return has_few(q, a.G) ? max(1, (q.len + p.tile_keys - 1) / p.tile_keys) : 0;
-}
-// First tile of workgroup w of n, and the workgroup that takes a tile.
-__device__ __forceinline__ uint32_t few_first(uint32_t total, int w, int n) { return (uint32_t)((uint64_t)total * w / n); }
-__device__ __forceinline__ int few_owner(uint32_t total, uint32_t tile, int n)
-{
-    return (int)((((uint64_t)tile + 1) * n - 1) / total);
 }
 
 // Many rows: blocks of R stacked rows of a head, and of the key tiles that each sees so many units of `step` tiles.  The units of
@@ -101,11 +119,9 @@ __device__ __forceinline__ int few_owner(uint32_t total, uint32_t tile, int n)
 // convex function of evenly spaced numbers is largest in sum at the ends, and rounding up adds less than 1 to either of two.)
 constexpr int kMostManyWorkgroups = 512;   // two a compute unit
 struct ManyPlan {
-    int n_wg, block_rows, tile_keys, step;
+    JoinPlan join;
+    int block_rows, tile_keys, step;
     int leave_few;    // sequences of few rows are the other kernel's
-    int blocks;       // at least the blocks of all sequences
-    int slot_floats;  // [block_rows, D] sums, [block_rows] maxima and sums of weights
-    float *slots;     // two a workgroup
 };
 struct ManySeq {
     int rows, blocks;        // stacked
@@ -131,23 +147,16 @@ __device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &
     m.per_head = m.blocks / 2 * m.pair + m.middle;
     return m;
 }
-// The first unit of block k, counted from the head's.
-__device__ __forceinline__ uint32_t many_start(const SeqRows &q, const ManySeq &m, int k, const AttendArgs &a, const ManyPlan &p)
-{
-    const int half = m.blocks / 2, mirror = m.blocks - 1 - k;
-    if (k >= half) return (uint32_t)mirror * m.pair;   // the later block of its pair, or the middle one
-    return (uint32_t)k * m.pair + many_units(q, m.rows, mirror, false, a, p);
-}
-
 // ---- launchers ------------------------------------------------------------------------------------------
 bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
 ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
-hipError_t launch_attend_join_few(const AttendArgs &a, const FewPlan &pl, int dtype, hipStream_t st);
 hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
-hipError_t launch_attend_join_many(const AttendArgs &a, const ManyPlan &pl, int dtype, hipStream_t st);
+hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &pl, int dtype, hipStream_t st);
+inline size_t join_record_bytes(const JoinPlan &p) { return (size_t)p.n_wg * sizeof(JoinRecord); }
+inline size_t join_slot_bytes(const JoinPlan &p) { return (size_t)2 * p.n_wg * p.slot_floats * 4; }
 
 // Head dimension that the matrix-core kernels fill d up to.
 inline int attend_width(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }

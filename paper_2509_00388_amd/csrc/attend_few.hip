@@ -37,12 +37,13 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     int n_wg = 0;
     int s = find_share(b.n_seqs, total, before, part, [&](int i) { return few_tiles(seq_rows(b, i), a, pl) * b.H; },
                        [&](uint32_t all) {
-                           n_wg = (int)min((uint32_t)pl.n_wg, all);
-                           return (int)blockIdx.x < n_wg ? (int64_t)few_first(all, blockIdx.x, n_wg) : -1;
+                           n_wg = (int)min((uint32_t)pl.join.n_wg, all);
+                           if (tid == 0) pl.join.records[blockIdx.x].parts = 0;
+                           return (int)blockIdx.x < n_wg ? (int64_t)stretch_first(all, blockIdx.x, n_wg) : -1;
                        });
     if (s < 0) return;
-    uint32_t tile = few_first(total, blockIdx.x, n_wg);
-    const uint32_t last = few_first(total, blockIdx.x + 1, n_wg), mine = tile;
+    uint32_t tile = stretch_first(total, blockIdx.x, n_wg);
+    const uint32_t last = stretch_first(total, blockIdx.x + 1, n_wg), mine = tile;
     const int pieces = b.d * L::kCached / 16, my_piece = lane % L::kPieces, my_row = lane / L::kPieces;
     const int load_piece = min(my_piece, pieces - 1);
 
@@ -181,8 +182,11 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
                         make_float4(o[x][4 * j] * f, o[x][4 * j + 1] * f, o[x][4 * j + 2] * f, o[x][4 * j + 3] * f);
         }
         const bool whole = t0 == 0 && t1 == (int)per_head;
-        float *slot = pl.slots + (size_t)(2 * blockIdx.x + (tile == mine ? 0 : 1)) * pl.slot_floats;
-        float *stat = slot + pl.slot_rows * D;
+        const int slot_at = 2 * blockIdx.x + (tile == mine ? 0 : 1);
+        if (tid == 0 && t0 == 0 && !whole)
+            pl.join.records[blockIdx.x] = {stretch_owner(total, tile + per_head - 1, n_wg) - (int)blockIdx.x + 1, slot_at, sq.row0, h, 0, rows};
+        float *slot = pl.join.slots + (size_t)slot_at * pl.join.slot_floats;
+        float *stat = slot + pl.join.slot_rows * D;
         float *sums = ml + 256 + 4 * rows * (D + 4);   // [rows]
         if (wv == 0 && hh == 0 && l32 < rows) {
             sums[l32] = sum;
@@ -212,67 +216,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     }
 }
 
-// The parts of pairs that several workgroups held: a workgroup a (row, query head).
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, FewPlan pl)
-{
-    constexpr int GROUPS = 256 / (D / 4);   // each takes every GROUPS-th part
-    __shared__ uint32_t part[16];
-    __shared__ float weight[kMostFewWorkgroups], red[16];
-    __shared__ float4 sums[GROUPS][D / 4];
-    const PagedBatch &b = a.b;
-    const int row = blockIdx.x, h = blockIdx.y / a.G, g = blockIdx.y % a.G, tid = threadIdx.x;
-    const int s = seq_of_row(b, row, tid & 63);
-    if (s >= b.n_seqs) return;
-    const SeqRows sq = seq_rows(b, s);
-    if (row < sq.row0 || row >= sq.row0 + sq.n) return;
-    const uint32_t per_head = few_tiles(sq, a, pl);
-    if (per_head == 0) return;
-    uint32_t before;
-    const uint32_t total = weigh(b.n_seqs, s, before, part, [&](int i) { return few_tiles(seq_rows(b, i), a, pl) * b.H; });
-    const int n_wg = (int)min((uint32_t)pl.n_wg, total);
-    const uint32_t first = before + h * per_head, end = first + per_head;
-    const int w0 = few_owner(total, first, n_wg), parts = min(few_owner(total, end - 1, n_wg), n_wg - 1) - w0 + 1;
-    if (parts <= 1) return;   // finished where it was computed
-    // (a workgroup that starts within this pair holds it in its first stretch, one that came from another pair in its last)
-    auto slot_of = [&](int w) {
-        return pl.slots + (size_t)(2 * w + (few_first(total, w, n_wg) >= first ? 0 : 1)) * pl.slot_floats;
-    };
-    const int r = (row - sq.row0) * a.G + g;
-    float top = -INFINITY, sum = 0.f;
-    for (int k = tid; k < parts; k += 256) {
-        weight[k] = slot_of(w0 + k)[pl.slot_rows * D + 2 * r];
-        top = fmaxf(top, weight[k]);
-    }
-    top = block_max(top, red);
-    const float shift = top == -INFINITY ? 0.f : top;
-    for (int k = tid; k < parts; k += 256) {
-        weight[k] = __builtin_amdgcn_exp2f(weight[k] - shift);
-        sum = fmaf(slot_of(w0 + k)[pl.slot_rows * D + 2 * r + 1], weight[k], sum);
-    }
-    sum = block_sum(sum, red);   // (its barriers: the weights are there)
-    const int c4 = tid % (D / 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int k = tid / (D / 4); k < parts; k += GROUPS) {
-        const float4 y = *reinterpret_cast<const float4 *>(slot_of(w0 + k) + r * D + 4 * c4);
-        const float f = weight[k];
-        v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-    }
-    sums[tid / (D / 4)][c4] = v;
-    __syncthreads();
-    if (a.lse && tid == 0) a.lse[(long)row * b.H * a.G + h * a.G + g] = lse_of(top, sum);
-    if (tid >= D / 4 || 4 * c4 >= b.d) return;
-    for (int k = 1; k < GROUPS; ++k) {
-        const float4 y = sums[k][c4];
-        v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
-    }
-    const float f = inverse_of(sum);
-    T *to = reinterpret_cast<T *>(a.out) + row * a.o_row + (h * a.G + g) * a.o_head + 4 * c4;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-    else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f));
-}
-
 // 32-key blocks of a wave's share of a tile: as many as put 8 KiB of keys in flight.
 template <typename T, int FORM, int D> constexpr int blocks_of() { return D <= 64 ? 2 : 1; }
 
@@ -282,11 +225,11 @@ hipError_t go_few(const AttendArgs &a, const FewPlan &pl, hipStream_t st)
     constexpr int NB = blocks_of<T, FORM, D>();
     using P = WavePlace<T, FORM, D, NB>;
     const int tiles = 4 * P::kBytes + 32 * P::kPitch;
-    const int joined = (256 + 4 * pl.slot_rows * (D + 4) + pl.slot_rows) * 4;
+    const int joined = (256 + 4 * pl.join.slot_rows * (D + 4) + pl.join.slot_rows) * 4;
     const int lds = tiles > joined ? tiles : joined;
     auto kernel = attend_few_kernel<T, FORM, D, NB>;
     if (lds > 64 * 1024 && !allow_big_lds(reinterpret_cast<const void *>(kernel))) return hipErrorInvalidValue;
-    kernel<<<pl.n_wg, 256, lds, st>>>(a, pl);
+    kernel<<<pl.join.n_wg, 256, lds, st>>>(a, pl);
     return hipGetLastError();
 }
 
@@ -308,10 +251,11 @@ FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G)
     FewPlan p{};
     p.tile_keys = 4 * 32 * (D <= 64 ? 2 : 1);
     const long rows = (long)b.max_rows * G;
-    p.slot_rows = rows < kFewRows ? (int)rows : kFewRows;
-    p.slot_floats = (p.slot_rows * (D + 2) + 3) & ~3;
+    p.join.slot_rows = rows < kFewRows ? (int)rows : kFewRows;
+    p.join.slot_floats = (p.join.slot_rows * (D + 2) + 3) & ~3;
+    p.join.rows_per_wg = 1;
     const long cap = (((long)b.table_pages << b.page_shift) + p.tile_keys - 1) / p.tile_keys * b.H * b.n_seqs;
-    p.n_wg = cap < kMostFewWorkgroups ? (int)cap : kMostFewWorkgroups;
+    p.join.n_wg = cap < kMostFewWorkgroups ? (int)cap : kMostFewWorkgroups;
     return p;
 }
 
@@ -322,16 +266,6 @@ hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, 
              : form == kPagesFp8   ? go_few_d<float, kPagesFp8>(a, pl, st) : go_few_d<float, kPagesInt8>(a, pl, st);
     return form == kPagesPlain ? go_few_d<uint16_t, kPagesPlain>(a, pl, st)
          : form == kPagesFp8   ? go_few_d<uint16_t, kPagesFp8>(a, pl, st) : go_few_d<uint16_t, kPagesInt8>(a, pl, st);
-}
-
-hipError_t launch_attend_join_few(const AttendArgs &a, const FewPlan &pl, int dtype, hipStream_t st)
-{
-    const dim3 grid(a.b.n_rows, a.b.H * a.G);
-    const int D = attend_width(a.b.d);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
-    if (dtype == 0)
-        return D == 64 ? go(attend_join_few_kernel<float, 64>) : go(attend_join_few_kernel<float, 128>);
-    return D == 64 ? go(attend_join_few_kernel<uint16_t, 64>) : D == 128 ? go(attend_join_few_kernel<uint16_t, 128>) : go(attend_join_few_kernel<uint16_t, 256>);
 }
 
 }  // namespace gkv

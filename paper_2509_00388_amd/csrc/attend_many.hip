@@ -30,20 +30,21 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     const PagedBatch &b = a.b;
 
     uint32_t total, before, pos = 0, last = 0;
+    int n_wg = 0, me = 0;
     int s = find_share(b.n_seqs, total, before, part, [&](int i) { return many_seq(seq_rows(b, i), a, pl).per_head * b.H; },
                        [&](uint32_t all) {
-                           const int n = (int)min((uint32_t)pl.n_wg, all), id = blockIdx.x;
-                           if (id >= n) return (int64_t)-1;
+                           const int id = blockIdx.x, xcd = id % 8;
+                           n_wg = (int)min((uint32_t)pl.join.n_wg, all);
                            // Neighbouring stretches, which read the same keys at about the same time, to one XCD's workgroups.
-                           const int xcd = id % 8, w = xcd * (n / 8) + min(xcd, n % 8) + id / 8;
-                           pos = few_first(all, w, n);
-                           last = few_first(all, w + 1, n);
+                           me = id < n_wg ? xcd * (n_wg / 8) + min(xcd, n_wg % 8) + id / 8 : id;
+                           if (tid == 0) pl.join.records[me].parts = 0;
+                           if (id >= n_wg) return (int64_t)-1;
+                           pos = stretch_first(all, me, n_wg);
+                           last = stretch_first(all, me + 1, n_wg);
                            return (int64_t)pos;
                        });
     if (s < 0) return;
     const uint32_t mine = pos;
-    const int n_wg = (int)min((uint32_t)pl.n_wg, total);
-    const int slot0 = 2 * ((int)(blockIdx.x % 8) * (n_wg / 8) + min((int)(blockIdx.x % 8), n_wg % 8) + (int)blockIdx.x / 8);
 
     const int pieces = b.d * L::kCached / 16, my_piece = tid % L::kPieces, my_row = tid / L::kPieces;
     const int wave_row = __builtin_amdgcn_readfirstlane(my_row);
@@ -206,10 +207,13 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             }
             __syncthreads();   // (the next block's tiles come to this place)
         }
+        if (tid == 0 && u0 == 0 && u1 < units)
+            pl.join.records[me] = {stretch_owner(total, pos + units - 1, n_wg) - me + 1, 2 * me + (pos == mine ? 0 : 1), sq.row0, h, row0,
+                                   min(R, ms.rows - row0)};
         const int r = 32 * group + l32;
         if (stream == 0 && row0 + r < ms.rows) {
             if (u0 > 0 || u1 < units) {
-                float *slot = pl.slots + (size_t)(slot0 + (pos == mine ? 0 : 1)) * pl.slot_floats;
+                float *slot = pl.join.slots + (size_t)(2 * me + (pos == mine ? 0 : 1)) * pl.join.slot_floats;
                 if (hh == 0) { slot[R * D + 2 * r] = m; slot[R * D + 2 * r + 1] = l; }
 #pragma unroll
                 for (int x = 0; x < DB; ++x)
@@ -240,61 +244,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     }
 }
 
-// The parts of blocks that several workgroups held: a workgroup 32 rows of a (block, head).
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_join_many_kernel(AttendArgs a, ManyPlan pl)
-{
-    __shared__ uint32_t part[16];
-    __shared__ float tops[32], sums[32];
-    const PagedBatch &b = a.b;
-    const int h = blockIdx.x % b.H, tid = threadIdx.x;
-    uint32_t blocks, first_block;
-    const int s = find_share(b.n_seqs, blocks, first_block, part, [&](int i) { return (uint32_t)many_seq(seq_rows(b, i), a, pl).blocks; },
-                             [&](uint32_t all) { return blockIdx.x / b.H < all ? (int64_t)(blockIdx.x / b.H) : (int64_t)-1; });
-    if (s < 0 || s >= b.n_seqs) return;
-    __syncthreads();
-    uint32_t before;
-    const uint32_t total = weigh(b.n_seqs, s, before, part, [&](int i) { return many_seq(seq_rows(b, i), a, pl).per_head * b.H; });
-    const SeqRows sq = seq_rows(b, s);
-    const ManySeq ms = many_seq(sq, a, pl);
-    const int block = (int)(blockIdx.x / b.H - first_block), r0 = 32 * blockIdx.y, rows = min(ms.rows - block * pl.block_rows - r0, 32);
-    if (rows <= 0) return;
-    const int n_wg = (int)min((uint32_t)pl.n_wg, total);
-    const uint32_t first = before + h * ms.per_head + many_start(sq, ms, block, a, pl);
-    const uint32_t end = first + many_units(sq, ms.rows, block, false, a, pl);
-    const int w0 = few_owner(total, first, n_wg), w1 = min(few_owner(total, end - 1, n_wg), n_wg - 1);
-    if (w0 >= w1) return;   // finished where it was computed
-    auto slot_of = [&](int w) { return pl.slots + (size_t)(2 * w + (few_first(total, w, n_wg) >= first ? 0 : 1)) * pl.slot_floats; };
-    const int stat = pl.block_rows * D;
-    if (tid < rows) {
-        float top = -INFINITY, sum = 0.f;
-        for (int w = w0; w <= w1; ++w) top = fmaxf(top, slot_of(w)[stat + 2 * (r0 + tid)]);
-        const float shift = top == -INFINITY ? 0.f : top;
-        for (int w = w0; w <= w1; ++w)
-            sum = fmaf(slot_of(w)[stat + 2 * (r0 + tid) + 1], __builtin_amdgcn_exp2f(slot_of(w)[stat + 2 * (r0 + tid)] - shift), sum);
-        tops[tid] = shift;
-        sums[tid] = inverse_of(sum);
-        const int stacked = block * pl.block_rows + r0 + tid;
-        if (a.lse) a.lse[(long)(sq.row0 + stacked / a.G) * b.H * a.G + h * a.G + stacked % a.G] = lse_of(top, sum);
-    }
-    __syncthreads();
-    for (int e = tid; e < rows * (D / 4); e += 256) {
-        const int r = e / (D / 4), c4 = 4 * (e % (D / 4)), stacked = block * pl.block_rows + r0 + r;
-        if (c4 >= b.d) continue;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int w = w0; w <= w1; ++w) {
-            const float *p = slot_of(w);
-            const float f = __builtin_amdgcn_exp2f(p[stat + 2 * (r0 + r)] - tops[r]);
-            const float4 y = *reinterpret_cast<const float4 *>(p + (r0 + r) * D + c4);
-            v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-        }
-        const float f = sums[r];
-        T *to = reinterpret_cast<T *>(a.out) + (sq.row0 + stacked / a.G) * a.o_row + (h * a.G + stacked % a.G) * a.o_head + c4;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f));
-    }
-}
-
 // Keys of a tile: 64, where the LDS holds two such tiles for two workgroups, otherwise 32.
 template <typename T, int D> constexpr int many_tile_keys() { return D * (int)sizeof(T) <= 256 ? 64 : 32; }
 
@@ -308,7 +257,7 @@ hipError_t go_many_rows(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
     const int lds = tiles > joined ? tiles : joined;
     auto kernel = attend_many_kernel<T, FORM, D, NB, RG>;
     if (lds > 64 * 1024 && !allow_big_lds(reinterpret_cast<const void *>(kernel))) return hipErrorInvalidValue;
-    kernel<<<pl.n_wg, 256, lds, st>>>(a, pl);
+    kernel<<<pl.join.n_wg, 256, lds, st>>>(a, pl);
     return hipGetLastError();
 }
 
@@ -337,16 +286,18 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
     p.leave_few = leave_few;
     p.tile_keys = D * (dtype == 0 ? 4 : 2) <= 256 ? 64 : 32;
     p.block_rows = p.tile_keys == 64 && (long)b.max_rows * G <= 64 ? 64 : 128;
-    p.blocks = (int)((long)b.n_rows * G / p.block_rows) + b.n_seqs;
-    p.slot_floats = p.block_rows * (D + 2);
+    p.join.slot_rows = p.block_rows;
+    p.join.slot_floats = p.block_rows * (D + 2);
+    p.join.rows_per_wg = 8;
+    const long blocks = (long)b.n_rows * G / p.block_rows + b.n_seqs;   // at least those of all sequences
     // Units of 256 keys, or more where their number could pass 31 bits.
     const long cap = (long)b.table_pages << b.page_shift;
     long units = 0;
     for (p.step = 256 / p.tile_keys;; p.step *= 2) {
-        units = ((long)p.blocks / 2 + b.n_seqs) * (2 * (cap / ((long)p.tile_keys * p.step) + 1) + 2) * b.H;
+        units = (blocks / 2 + b.n_seqs) * (2 * (cap / ((long)p.tile_keys * p.step) + 1) + 2) * b.H;
         if (units <= INT32_MAX) break;
     }
-    p.n_wg = units < kMostManyWorkgroups ? (int)units : kMostManyWorkgroups;
+    p.join.n_wg = units < kMostManyWorkgroups ? (int)units : kMostManyWorkgroups;
     return p;
 }
 
@@ -357,16 +308,6 @@ hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype
              : form == kPagesFp8   ? go_many_d<float, kPagesFp8>(a, pl, st) : go_many_d<float, kPagesInt8>(a, pl, st);
     return form == kPagesPlain ? go_many_d<uint16_t, kPagesPlain>(a, pl, st)
          : form == kPagesFp8   ? go_many_d<uint16_t, kPagesFp8>(a, pl, st) : go_many_d<uint16_t, kPagesInt8>(a, pl, st);
-}
-
-hipError_t launch_attend_join_many(const AttendArgs &a, const ManyPlan &pl, int dtype, hipStream_t st)
-{
-    const dim3 grid(pl.blocks * a.b.H, pl.block_rows / 32);
-    const int D = attend_width(a.b.d);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
-    if (dtype == 0)
-        return D == 64 ? go(attend_join_many_kernel<float, 64>) : go(attend_join_many_kernel<float, 128>);
-    return D == 64 ? go(attend_join_many_kernel<uint16_t, 64>) : D == 128 ? go(attend_join_many_kernel<uint16_t, 128>) : go(attend_join_many_kernel<uint16_t, 256>);
 }
 
 }  // namespace gkv

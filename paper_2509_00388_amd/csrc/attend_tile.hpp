@@ -49,7 +49,7 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
     static constexpr int kPieces = D * kCached / 16;                             // 16-byte pieces of a cached row
     static constexpr int kPer = KEYS * kPieces / NT;                             // pieces of a thread
     static constexpr int kRowStep = NT / kPieces;                                // rows between two of its pieces
-    static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + 32;
+    static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 32);
     static constexpr int kDecoded = 16 / kCached * (int)sizeof(T);               // bytes of a piece in the LDS
     static constexpr int kSteps = D * (int)sizeof(T) / 32;                       // matrix steps of a row of keys
     static_assert(KEYS * kPieces % NT == 0 && NT % kPieces == 0, "whole rows a turn");
