@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libgraphkv.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["api.hip", "select.hip", "generic.hip", "gemm.hip", "stages.hip", "mfma_score.hip", "mfma_cosine.hip",
-           "cache.hip", "attend.hip", "attend_few.hip", "attend_many.hip"]
+           "cache.hip", "attend.hip", "attend_few.hip", "attend_many.hip", "attend_wide.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", 

@@ -372,7 +372,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     // (key tiles of all sequences and heads, and the workgroups of the largest launch, are counted in 32 bits)
     const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
     if (((tokens + 127) / 128) * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
-    if (((int64_t)p->n_rows * A.G / 64 + p->n_seqs) * p->n_kv_heads > INT32_MAX) return false;
+    if ((int64_t)p->n_rows * A.G > (1 << 30)) return false;   // (and so are stacked rows)
     // Sequences of few rows and of many are different kernels' where both can occur; a batch of one sequence is one or the other.
     A.many = (int64_t)b.max_rows * A.G > kFewRows;
     A.few = !A.many || b.n_seqs > 1;
@@ -920,7 +920,8 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
     if (A.many) {
         A.mp.join.records = at<JoinRecord>(ws, A.many_records);
         A.mp.join.slots = at<float>(ws, A.many_slots);
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, st)
+                                                    : launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
         GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.mp.join, p->dtype, st));
     }
     return GRAPHKV_OK;

@@ -25,53 +25,48 @@ __device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1
 
 // ---- how work is cut ----------------------------------------------------------------------------------
 // The lengths are known to the device alone, so each workgroup adds up for itself what lies before its share.  `weight(s)` is
-// the work of sequence s in whatever unit; workgroups of 256 threads, `part`: 16 words of LDS.
-template <typename W> __device__ uint32_t weigh(int n_seqs, int of, uint32_t &before, uint32_t *part, W &&weight)
+// the work of sequence s in whatever unit; workgroups of NW waves, `part`: 20 words of LDS.
+template <int NW, typename W> __device__ uint32_t weigh(int n_seqs, uint32_t *part, W &&weight)
 {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     uint32_t total = 0;
-    before = 0;
-    for (int first = 0; first < n_seqs; first += 256) {
+    for (int first = 0; first < n_seqs; first += 64 * NW) {
         const int s = first + tid;
-        const uint32_t w = s < n_seqs ? weight(s) : 0;
-        const uint32_t all = wave_sum_u32(w), some = wave_sum_u32(s < of ? w : 0u);
+        const uint32_t all = wave_sum_u32(s < n_seqs ? weight(s) : 0u);
         __syncthreads();
-        if (lane == 0) { part[wv] = all; part[4 + wv] = some; }
+        if (lane == 0) part[wv] = all;
         __syncthreads();
-        total += part[0] + part[1] + part[2] + part[3];
-        before += part[4] + part[5] + part[6] + part[7];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) total += part[w];
     }
     return total;
 }
 // The sequence that holds unit `first(total)` (below the total), the units before it and the total; -1 if first() says so.
-template <typename W, typename F>
+template <int NW, typename W, typename F>
 __device__ int find_share(int n_seqs, uint32_t &total, uint32_t &before, uint32_t *part, W &&weight, F &&first)
 {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     uint32_t w = tid < n_seqs ? weight(tid) : 0;
-    if (tid == 0) part[10] = (uint32_t)n_seqs;   // (found nowhere: only where row numbers that do not ascend overflow the sums)
-    uint32_t at = block_scan_add<4>(w, part, lane, wv, total);
-    if (n_seqs > 256) {   // (more sequences than threads: the total in a pass of its own)
-        uint32_t none;
-        total = weigh(n_seqs, 0, none, part, weight);
-    }
+    if (tid == 0) part[16] = (uint32_t)n_seqs;   // (found nowhere: only where row numbers that do not ascend overflow the sums)
+    uint32_t at = block_scan_add<NW>(w, part, lane, wv, total);
+    if (n_seqs > 64 * NW) total = weigh<NW>(n_seqs, part, weight);   // (more sequences than threads: in a pass of its own)
     const int64_t unit = first(total);
     if (unit < 0) return -1;
-    for (int s0 = 0; ; s0 += 256) {
+    for (int s0 = 0; ; s0 += 64 * NW) {
         if (s0 > 0) {
             uint32_t here;
-            const uint32_t base = part[12];
+            const uint32_t base = part[18];
             w = s0 + tid < n_seqs ? weight(s0 + tid) : 0;
             __syncthreads();
-            at = base + block_scan_add<4>(w, part, lane, wv, here);
+            at = base + block_scan_add<NW>(w, part, lane, wv, here);
         }
-        if (unit >= at && unit < (int64_t)at + w) { part[10] = (uint32_t)(s0 + tid); part[11] = at; }
-        if (tid == 255) part[12] = at + w;
+        if (unit >= at && unit < (int64_t)at + w) { part[16] = (uint32_t)(s0 + tid); part[17] = at; }
+        if (tid == 64 * NW - 1) part[18] = at + w;
         __syncthreads();
-        if (unit < (int64_t)part[12] || s0 + 256 >= n_seqs) break;
+        if (unit < (int64_t)part[18] || s0 + 64 * NW >= n_seqs) break;
     }
-    before = part[11];
-    return __builtin_amdgcn_readfirstlane((int)part[10]);
+    before = part[17];
+    return __builtin_amdgcn_readfirstlane((int)part[16]);
 }
 
 // Equal stretches of `total` units for n workgroups: the first unit of the w-th, and the one that takes a unit.
@@ -117,24 +112,24 @@ __device__ __forceinline__ uint32_t few_tiles(const SeqRows &q, const AttendArgs
 // units are nearly the same number: a pair gets room for W = units(first) + units(last) + 2 of them, what is left of it is
 // empty.  (Units u of a block that sees e keys are max(1, ceil(e / K)); e grows evenly up to rounding down by less than 1, a
 // convex function of evenly spaced numbers is largest in sum at the ends, and rounding up adds less than 1 to either of two.)
-constexpr int kMostManyWorkgroups = 512;   // two a compute unit
 struct ManyPlan {
     JoinPlan join;
     int block_rows, tile_keys, step;
     int leave_few;    // sequences of few rows are the other kernel's
+    int wide;         // blocks of 256 rows (attend_wide.hip)
 };
 struct ManySeq {
     int rows, blocks;        // stacked
     uint32_t pair, middle;   // units of a pair of blocks, of the block that is left in the middle
     uint32_t per_head;
 };
-// Units of block k of a sequence; `whole`: as if it were full of rows.
+// Units of block k of a sequence; `whole`: as if it were full of rows.  (Stacked rows and positions are below 2^31 together.)
 __device__ __forceinline__ uint32_t many_units(const SeqRows &q, int rows, int k, bool whole, const AttendArgs &a, const ManyPlan &p)
 {
-    const long end = (long)(k + 1) * p.block_rows;
-    const long sees = (long)q.len - q.n + ((whole ? end : min(end, (long)rows)) - 1) / a.G + 1;
-    const long keys = (long)p.tile_keys * p.step;
-    return sees <= keys ? 1u : (uint32_t)((sees + keys - 1) / keys);
+    const uint32_t end = (uint32_t)(k + 1) * p.block_rows;
+    const int sees = q.len - q.n + (int)(((whole ? end : min(end, (uint32_t)rows)) - 1) / (uint32_t)a.G) + 1;
+    const uint32_t keys = (uint32_t)p.tile_keys * p.step;
+    return sees <= (int)keys ? 1u : ((uint32_t)sees + keys - 1) / keys;
 }
 __device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &a, const ManyPlan &p)
 {
@@ -147,6 +142,46 @@ __device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &
     m.per_head = m.blocks / 2 * m.pair + m.middle;
     return m;
 }
+// The next part of a stretch pos .. last - 1: units u0 .. u1 - 1 of a block's `units`.  False at the stretch's end.
+struct ManyPart {
+    SeqRows sq;
+    int rows, h, block;   // rows: stacked rows of the sequence
+    uint32_t u0, u1, units;
+};
+__device__ __forceinline__ bool next_part(const AttendArgs &a, const ManyPlan &pl, uint32_t &pos, uint32_t last, int &s,
+                                          uint32_t &before, ManyPart &p)
+{
+    while (pos < last && s < a.b.n_seqs) {
+        p.sq = seq_rows(a.b, s);
+        const ManySeq ms = many_seq(p.sq, a, pl);
+        if (ms.per_head == 0 || pos >= before + ms.per_head * a.b.H) {   // the next sequence
+            before += ms.per_head * a.b.H;
+            ++s;
+            continue;
+        }
+        p.rows = ms.rows;
+        p.h = (int)((pos - before) / ms.per_head);
+        uint32_t at = (pos - before) % ms.per_head;
+        const int pair = ms.pair ? (int)min(at / ms.pair, (uint32_t)ms.blocks / 2) : 0;
+        at -= (uint32_t)pair * ms.pair;
+        p.u0 = at;
+        p.block = ms.blocks - 1 - pair;
+        p.units = many_units(p.sq, p.rows, p.block, false, a, pl);
+        if (p.u0 >= p.units) {
+            p.u0 -= p.units;
+            p.block = pair;
+            p.units = many_units(p.sq, p.rows, pair, false, a, pl);
+            if (p.u0 >= p.units) {   // the pair's empty rest
+                pos += ms.pair - at;
+                continue;
+            }
+        }
+        p.u1 = min(p.units, p.u0 + (last - pos));
+        return true;
+    }
+    return false;
+}
+
 // ---- launchers ------------------------------------------------------------------------------------------
 bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
@@ -154,6 +189,7 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_attend_wide(const AttendArgs &a, const ManyPlan &pl, int form, hipStream_t st);
 hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &pl, int dtype, hipStream_t st);
 inline size_t join_record_bytes(const JoinPlan &p) { return (size_t)p.n_wg * sizeof(JoinRecord); }
 inline size_t join_slot_bytes(const JoinPlan &p) { return (size_t)2 * p.n_wg * p.slot_floats * 4; }

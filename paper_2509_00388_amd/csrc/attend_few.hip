@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     using P = WavePlace<T, FORM, D, NB>;
     constexpr uint64_t kAllKeys = KEYS == 64 ? ~0ull : (1ull << KEYS) - 1;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ uint32_t part[16];
+    __shared__ uint32_t part[20];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
     unsigned char *kv = smem + wv * P::kBytes, *qt = smem + 4 * P::kBytes;
     float *ks = reinterpret_cast<float *>(kv + P::kRows), *vs = ks + KEYS;
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
 
     uint32_t total, before;
     int n_wg = 0;
-    int s = find_share(b.n_seqs, total, before, part, [&](int i) { return few_tiles(seq_rows(b, i), a, pl) * b.H; },
+    int s = find_share<4>(b.n_seqs, total, before, part, [&](int i) { return few_tiles(seq_rows(b, i), a, pl) * b.H; },
                        [&](uint32_t all) {
                            n_wg = (int)min((uint32_t)pl.join.n_wg, all);
                            if (tid == 0) pl.join.records[blockIdx.x].parts = 0;
@@ -63,9 +63,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         const int my_key = wv * KEYS + (lane & (KEYS - 1));
         auto entry = [&](int t) {   // page of the lane's key in tile t, -1: none
             const int pos = t * pl.tile_keys + my_key;
-            return t < t1 && pos < sq.len ? page_of(b, s, pos) : -1;
+            return t < t1 && pos < sq.len ? raw_page(b, s, pos) : -1;
         };
-        auto place = [&](int page, int t) { return page < 0 ? 0 : pool_row(b, page, h, t * pl.tile_keys + my_key); };
+        auto place = [&](int page, int t) { return !is_page(b, page) ? 0 : pool_row(b, page, h, t * pl.tile_keys + my_key); };
         uint4 kr[L::kPer], vr[L::kPer];
         float ksr = 0.f, vsr = 0.f;
         auto load = [&](const void *pages, int at, uint4 (&r)[L::kPer]) {
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             }
         };
         int page = entry(t0), at = place(page, t0);
-        uint64_t vis = __ballot(page >= 0) & kAllKeys;
+        uint64_t vis = __ballot(is_page(b, page)) & kAllKeys;
         load(a.Kpages, at, kr);
         if (FORM != kPagesPlain) { ksr = a.Kscale[at]; vsr = a.Vscale[at]; }
         load(a.Vpages, at, vr);
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
 
         for (int t = t0; t < t1; ++t) {   // in the registers: vis, at, page, kr, vr
             const int page2 = entry(t + 2), at1 = place(page1, t + 1);
-            const uint64_t vis1 = __ballot(page1 >= 0) & kAllKeys;
+            const uint64_t vis1 = __ballot(is_page(b, page1)) & kAllKeys;
             const int first = t * pl.tile_keys + wv * KEYS;
             const bool all = vis == kAllKeys && first + KEYS - 1 <= sq.len - sq.n;   // every row sees every key
             auto store = [&](const uint4 (&r)[L::kPer], uint64_t seen) {
@@ -118,8 +118,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             store(kr, vis >> my_row);
             if (FORM != kPagesPlain) {
                 if (lane < KEYS) {   // (a scale without a key may be anything too)
-                    ks[lane] = page >= 0 ? ksr * a.c : 0.f;
-                    vs[lane] = page >= 0 ? vsr : 0.f;
+                    ks[lane] = is_page(b, page) ? ksr * a.c : 0.f;
+                    vs[lane] = is_page(b, page) ? vsr : 0.f;
                 }
                 ksr = a.Kscale[at1];
                 vsr = a.Vscale[at1];

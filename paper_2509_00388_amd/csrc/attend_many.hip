@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     constexpr int KEYTILE = KEYS * L::kKeyPitch, HALF = KEYTILE + KEYS * L::kValPitch + (FORM == kPagesPlain ? 0 : 2 * KEYS * 4);
     constexpr uint64_t kAllKeys = KEYS == 64 ? ~0ull : (1ull << KEYS) - 1;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ uint32_t part[16];
+    __shared__ uint32_t part[20];
     __shared__ unsigned long long odd_of[3];   // rows of the tile before, of this one and of the next that hold infinities or NaN
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
     const int group = wv % RG, stream = wv / RG, key0 = 32 * NB * stream;   // the wave's rows of the block, its first key of a tile
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
 
     uint32_t total, before, pos = 0, last = 0;
     int n_wg = 0, me = 0;
-    int s = find_share(b.n_seqs, total, before, part, [&](int i) { return many_seq(seq_rows(b, i), a, pl).per_head * b.H; },
+    int s = find_share<4>(b.n_seqs, total, before, part, [&](int i) { return many_seq(seq_rows(b, i), a, pl).per_head * b.H; },
                        [&](uint32_t all) {
                            const int id = blockIdx.x, xcd = id % 8;
                            n_wg = (int)min((uint32_t)pl.join.n_wg, all);
@@ -52,38 +52,19 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     const bool pad = my_piece >= pieces;
     const int my_key = lane & (KEYS - 1);   // lane j of each wave looks key j of a tile up
 
-    while (pos < last && s < b.n_seqs) {
-        const SeqRows sq = seq_rows(b, s);
-        const ManySeq ms = many_seq(sq, a, pl);
-        if (ms.per_head == 0 || pos >= before + ms.per_head * b.H) {   // the next sequence
-            before += ms.per_head * b.H;
-            ++s;
-            continue;
-        }
-        const int h = (int)((pos - before) / ms.per_head);
-        uint32_t u0 = (pos - before) % ms.per_head;
-        const int pair = ms.pair ? (int)min(u0 / ms.pair, (uint32_t)ms.blocks / 2) : 0;
-        u0 -= (uint32_t)pair * ms.pair;
-        int block = ms.blocks - 1 - pair;
-        uint32_t units = many_units(sq, ms.rows, block, false, a, pl);
-        if (u0 >= units) {
-            u0 -= units;
-            block = pair;
-            units = many_units(sq, ms.rows, block, false, a, pl);
-            if (u0 >= units) {   // the pair's empty rest
-                pos += ms.pair - (ms.pair ? (pos - before) % ms.per_head % ms.pair : 0);
-                continue;
-            }
-        }
-        const uint32_t u1 = min(units, u0 + (last - pos));
-        const int row0 = block * R;                                                  // stacked rows of the sequence
+    ManyPart mp;
+    while (next_part(a, pl, pos, last, s, before, mp)) {
+        const SeqRows sq = mp.sq;
+        const int h = mp.h, rows = mp.rows;
+        const uint32_t u0 = mp.u0, u1 = mp.u1, units = mp.units;
+        const int row0 = mp.block * R;                                                  // stacked rows of the sequence
         const int row = row0 + 32 * group + l32;
         const int sees = sq.len - sq.n + row / a.G;                                  // last position the lane's row sees
-        const int extent = max(0, sq.len - sq.n + (min(row0 + R, ms.rows) - 1) / a.G + 1);   // positions the block sees
+        const int extent = max(0, sq.len - sq.n + (min(row0 + R, rows) - 1) / a.G + 1);   // positions the block sees
         const int first_sees = sq.len - sq.n + row0 / a.G;                           // last position that all its rows see
         const int t0 = (int)u0 * pl.step, t1 = min((int)u1 * pl.step, (extent + KEYS - 1) / KEYS);
 
-        const T *qrow = row < ms.rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / a.G) * a.q_row + (h * a.G + row % a.G) * a.q_head
+        const T *qrow = row < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / a.G) * a.q_row + (h * a.G + row % a.G) * a.q_head
                                       : nullptr;
         uint4 q[L::kSteps];
         load_query<T>(qrow, b.d, hh, q);
@@ -97,9 +78,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
 
         auto entry = [&](int t) {
             const int at = t * KEYS + my_key;
-            return t < t1 && at < extent ? page_of(b, s, at) : -1;
+            return t < t1 && at < extent ? raw_page(b, s, at) : -1;
         };
-        auto place = [&](int page, int t) { return page < 0 ? 0 : pool_row(b, page, h, t * KEYS + my_key); };
+        auto place = [&](int page, int t) { return !is_page(b, page) ? 0 : pool_row(b, page, h, t * KEYS + my_key); };
         uint4 kr[L::kPer], vr[L::kPer];
         float ksr = 0.f, vsr = 0.f;
         auto load = [&](int at) {
@@ -128,20 +109,20 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             }
             if (FORM != kPagesPlain && wv == 0 && lane < KEYS) {
                 float *ks = reinterpret_cast<float *>(smem + (t & 1) * HALF + KEYTILE + KEYS * L::kValPitch);
-                ks[lane] = page >= 0 ? ksr * a.c : 0.f;
-                ks[KEYS + lane] = page >= 0 ? vsr : 0.f;
+                ks[lane] = is_page(b, page) ? ksr * a.c : 0.f;
+                ks[KEYS + lane] = is_page(b, page) ? vsr : 0.f;
             }
         };
         if (tid < 3) odd_of[tid] = 0;
         int page = entry(t0), at = place(page, t0), page1 = entry(t0 + 1);
-        uint64_t vis = __ballot(page >= 0) & kAllKeys;
+        uint64_t vis = __ballot(is_page(b, page)) & kAllKeys;
         load(at);
         __syncthreads();
         store(t0, page, vis);
         __syncthreads();
         for (int t = t0; t < t1; ++t) {
             const int at1 = place(page1, t + 1), page2 = entry(t + 2);
-            const uint64_t vis1 = __ballot(page1 >= 0) & kAllKeys;
+            const uint64_t vis1 = __ballot(is_page(b, page1)) & kAllKeys;
             load(at1);
             const unsigned char *kt = smem + (t & 1) * HALF + key0 * L::kKeyPitch, *vt = smem + (t & 1) * HALF + KEYTILE + key0 * L::kValPitch;
             const float *ks = reinterpret_cast<const float *>(smem + (t & 1) * HALF + KEYTILE + KEYS * L::kValPitch) + key0;
@@ -209,9 +190,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         }
         if (tid == 0 && u0 == 0 && u1 < units)
             pl.join.records[me] = {stretch_owner(total, pos + units - 1, n_wg) - me + 1, 2 * me + (pos == mine ? 0 : 1), sq.row0, h, row0,
-                                   min(R, ms.rows - row0)};
+                                   min(R, rows - row0)};
         const int r = 32 * group + l32;
-        if (stream == 0 && row0 + r < ms.rows) {
+        if (stream == 0 && row0 + r < rows) {
             if (u0 > 0 || u1 < units) {
                 float *slot = pl.join.slots + (size_t)(2 * me + (pos == mine ? 0 : 1)) * pl.join.slot_floats;
                 if (hh == 0) { slot[R * D + 2 * r] = m; slot[R * D + 2 * r + 1] = l; }
@@ -285,7 +266,9 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
     ManyPlan p{};
     p.leave_few = leave_few;
     p.tile_keys = D * (dtype == 0 ? 4 : 2) <= 256 ? 64 : 32;
-    p.block_rows = p.tile_keys == 64 && (long)b.max_rows * G <= 64 ? 64 : 128;
+    const long most_rows = (long)b.max_rows * G;
+    p.wide = dtype != 0 && D <= 128 && most_rows > 128;
+    p.block_rows = p.wide ? 256 : p.tile_keys == 64 && most_rows <= 64 ? 64 : 128;
     p.join.slot_rows = p.block_rows;
     p.join.slot_floats = p.block_rows * (D + 2);
     p.join.rows_per_wg = 8;
@@ -295,9 +278,10 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
     long units = 0;
     for (p.step = 256 / p.tile_keys;; p.step *= 2) {
         units = (blocks / 2 + b.n_seqs) * (2 * (cap / ((long)p.tile_keys * p.step) + 1) + 2) * b.H;
-        if (units <= INT32_MAX) break;
+        if (units <= INT32_MAX || p.tile_keys * p.step >= 1 << 29) break;
     }
-    p.join.n_wg = units < kMostManyWorkgroups ? (int)units : kMostManyWorkgroups;
+    const int most = p.wide ? 256 : 512;   // one or two workgroups a compute unit
+    p.join.n_wg = units < most ? (int)units : most;
     return p;
 }
 

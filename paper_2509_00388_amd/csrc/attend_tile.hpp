@@ -47,12 +47,13 @@ __device__ __forceinline__ float other_half_sum(float x)
 template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
     static constexpr int kCached = FORM == kPagesPlain ? (int)sizeof(T) : 1;   // bytes of a cached value
     static constexpr int kPieces = D * kCached / 16;                             // 16-byte pieces of a cached row
-    static constexpr int kPer = KEYS * kPieces / NT;                             // pieces of a thread
+    static constexpr int kPer = (KEYS * kPieces + NT - 1) / NT;                  // pieces of a thread
+    static constexpr bool kSpare = KEYS * kPieces < NT;                          // threads without one
     static constexpr int kRowStep = NT / kPieces;                                // rows between two of its pieces
     static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 32);
     static constexpr int kDecoded = 16 / kCached * (int)sizeof(T);               // bytes of a piece in the LDS
     static constexpr int kSteps = D * (int)sizeof(T) / 32;                       // matrix steps of a row of keys
-    static_assert(KEYS * kPieces % NT == 0 && NT % kPieces == 0, "whole rows a turn");
+    static_assert((kSpare || KEYS * kPieces % NT == 0) && NT % kPieces == 0, "whole rows a turn");
 
     // Whether a piece holds an infinity or a NaN.
     __device__ static __forceinline__ bool odd(const uint4 &v)
@@ -119,27 +120,44 @@ __device__ __forceinline__ void load_query(const T *row, int d, int hh, uint4 (&
     }
 }
 
-// O^T += V^T P^T over a block of 32 keys: vt is the block's first row of values in the LDS, p the lane's 16 weights.
-template <int D, int PITCH>
-__device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], uint16_t)
+// A lane's weights of a block of 32 keys in bf16, as operands of two matrix steps.
+struct Weights {
+    bf16x8 w[2];
+};
+__device__ __forceinline__ Weights pack_weights(const float (&p)[16])
 {
-    const int i = lane & 15, hh = lane >> 5;
-    const unsigned char *at = vt + (4 * hh + (i >> 2)) * PITCH + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+    Weights r;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         union { uint4 u; bf16x8 v; } w;
         w.u = make_uint4(pack_bf16(p[8 * s], p[8 * s + 1]), pack_bf16(p[8 * s + 2], p[8 * s + 3]),
                          pack_bf16(p[8 * s + 4], p[8 * s + 5]), pack_bf16(p[8 * s + 6], p[8 * s + 7]));
+        r.w[s] = w.v;
+    }
+    return r;
+}
+
+// O^T += V^T P^T over a block of 32 keys: vt is the block's first row of values in the LDS.
+template <int D, int PITCH>
+__device__ __forceinline__ void add_values(const unsigned char *vt, const Weights &p, int lane, f32x16 (&o)[D / 32])
+{
+    const int i = lane & 15, hh = lane >> 5;
+    const unsigned char *at = vt + (4 * hh + (i >> 2)) * PITCH + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int b = 0; b < D / 32; ++b) {
             // two groups of four keys, as acc_row() deals them out
             typedef __attribute__((address_space(3))) bf16x4 lds4;
             const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + 16 * s * PITCH + 64 * b));
             const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + (16 * s + 8) * PITCH + 64 * b));
-            const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w.v, o[b], 0, 0, 0);
+            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p.w[s], o[b], 0, 0, 0);
         }
-    }
+}
+template <int D, int PITCH>
+__device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], uint16_t)
+{
+    add_values<D, PITCH>(vt, pack_weights(p), lane, o);
 }
 template <int D, int PITCH>
 __device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], float)

@@ -47,6 +47,13 @@ __device__ __forceinline__ int page_of(const PagedBatch &b, int s, int pos)
     const int page = b.table[(long)s * b.table_pages + (pos >> b.page_shift)];
     return (unsigned)page < (unsigned)b.n_pages ? page : -1;
 }
+// The table's entry as it is, for kernels that ask for it long before they use it: the comparison that page_of() makes would wait
+// for it, and for every load asked for before it.
+__device__ __forceinline__ int raw_page(const PagedBatch &b, int s, int pos)
+{
+    return b.table[(long)s * b.table_pages + (pos >> b.page_shift)];
+}
+__device__ __forceinline__ bool is_page(const PagedBatch &b, int page) { return (unsigned)page < (unsigned)b.n_pages; }
 __device__ __forceinline__ int pool_row(const PagedBatch &b, int page, int h, int pos)
 {
     return ((page * b.H + h) << b.page_shift) + (pos & ((1 << b.page_shift) - 1));
