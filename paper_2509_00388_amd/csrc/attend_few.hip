@@ -93,6 +93,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         __syncthreads();
         const int sees = sq.len - sq.n + l32 / a.G;   // last position that the lane's query, stacked row l32, sees
 
+        uint64_t odd_of[2] = {0, 0};   // of the first tile that not all rows see all of, and the next: values with infinities or NaN
+        const int hidden = max(0, sq.len - sq.n + 1) / pl.tile_keys;
+
         float m = -INFINITY, l = 0.f;
         f32x16 o[DB];
 #pragma unroll
@@ -138,7 +141,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             }
             wave_sync();
             uint64_t odd = 0;
-            if (!all) odd = L::odd_rows(vr, 0) & vis;
+            if (first + KEYS - 1 > sq.len - sq.n) {   // (no more than two of a wave's tiles)
+                odd = L::odd_rows(vr, 0) & vis;
+                odd_of[t > hidden] = odd;
+            }
             store(vr, (vis & ~odd) >> my_row);
             load(a.Vpages, at1, vr);
             float p[NB][16];
@@ -148,7 +154,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             wave_sync();
 #pragma unroll
             for (int n = 0; n < NB; ++n) add_values<D, P::kPitch>(kv + 32 * n * P::kPitch, p[n], lane, o, T{});
-            if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, 0, b.d, p, sees - first, lane, o);
             wave_sync();
             vis = vis1;
             at = at1;
@@ -160,6 +165,11 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         l = other_half_sum(l);
         int G = a.G;
         asm volatile("" : "+s"(G));   // (what was computed from it before the loop is not kept through it)
+        if (FORM != kPagesInt8 && (odd_of[0] | odd_of[1]))
+            for (int k = 0; k < 2; ++k)
+                add_odd_rows<T, FORM, DB>(a, s, h, k ? odd_of[1] : odd_of[0], (hidden + k) * pl.tile_keys + wv * KEYS,
+                                          l32 < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + l32 / G) * a.q_row + (h * G + l32 % G) * a.q_head : nullptr,
+                                          sq.len - sq.n + l32 / G, m, hh, o);
         __syncthreads();
         float *ml = reinterpret_cast<float *>(smem), *parts = ml + 256;   // [4][32][2], [4][rows][D + 4]
         if (hh == 0) { ml[(wv * 32 + l32) * 2] = m; ml[(wv * 32 + l32) * 2 + 1] = l; }

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     constexpr uint64_t kAllKeys = KEYS == 64 ? ~0ull : (1ull << KEYS) - 1;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ uint32_t part[20];
-    __shared__ unsigned long long odd_of[3];   // rows of the tile before, of this one and of the next that hold infinities or NaN
+    __shared__ unsigned long long odd_of[8];   // of the tiles that some rows do not see all of: values with infinities or NaN
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
     const int group = wv % RG, stream = wv / RG, key0 = 32 * NB * stream;   // the wave's rows of the block, its first key of a tile
     const PagedBatch &b = a.b;
@@ -62,12 +62,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         const int sees = sq.len - sq.n + row / a.G;                                  // last position the lane's row sees
         const int extent = max(0, sq.len - sq.n + (min(row0 + R, rows) - 1) / a.G + 1);   // positions the block sees
         const int first_sees = sq.len - sq.n + row0 / a.G;                           // last position that all its rows see
+        const int hidden = max(0, first_sees + 1) / KEYS;                            // the first tile that not all of them see all of
         const int t0 = (int)u0 * pl.step, t1 = min((int)u1 * pl.step, (extent + KEYS - 1) / KEYS);
 
-        const T *qrow = row < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / a.G) * a.q_row + (h * a.G + row % a.G) * a.q_head
-                                      : nullptr;
+        auto query = [&](int G) {
+            return row < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / G) * a.q_row + (h * G + row % G) * a.q_head : nullptr;
+        };
         uint4 q[L::kSteps];
-        load_query<T>(qrow, b.d, hh, q);
+        load_query<T>(query(a.G), b.d, hh, q);
 
         float m = -INFINITY, l = 0.f;
         f32x16 o[DB];
@@ -98,7 +100,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             uint64_t odd = 0;
             if (t * KEYS + KEYS - 1 > first_sees) {   // some rows do not see all of it
                 odd = L::odd_rows(vr, wave_row) & vis;
-                if (odd && lane == 0) atomicOr(&odd_of[t % 3], (unsigned long long)odd);
+                if (odd && lane == 0) atomicOr(&odd_of[t - hidden], (unsigned long long)odd);
             }
             // (places that hold no key of the sequence may hold anything: zeros instead)
             const uint64_t kseen = pad ? 0 : vis >> my_row, vseen = pad ? 0 : (vis & ~odd) >> my_row;
@@ -113,7 +115,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
                 ks[KEYS + lane] = is_page(b, page) ? vsr : 0.f;
             }
         };
-        if (tid < 3) odd_of[tid] = 0;
+        __syncthreads();   // (the part before is done with them)
+        if (tid < 8) odd_of[tid] = 0;
         int page = entry(t0), at = place(page, t0), page1 = entry(t0 + 1);
         uint64_t vis = __ballot(is_page(b, page)) & kAllKeys;
         load(at);
@@ -126,8 +129,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             load(at1);
             const unsigned char *kt = smem + (t & 1) * HALF + key0 * L::kKeyPitch, *vt = smem + (t & 1) * HALF + KEYTILE + key0 * L::kValPitch;
             const float *ks = reinterpret_cast<const float *>(smem + (t & 1) * HALF + KEYTILE + KEYS * L::kValPitch) + key0;
-            const uint64_t odd = odd_of[t % 3] >> key0 & (~0ull >> (64 - 32 * NB));
-            if (tid == 0) odd_of[(t + 2) % 3] = 0;   // (its readers are behind the last barrier, its next writers behind the next)
             const bool all = vis == kAllKeys && t * KEYS + KEYS - 1 <= first_sees;
             f32x16 x[NB];
 #pragma unroll
@@ -145,7 +146,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
             if constexpr (FORM != kPagesPlain) scale_weights<NB>(ks + KEYS, all, seen, hh, p);
 #pragma unroll
             for (int n = 0; n < NB; ++n) add_values<D, L::kValPitch>(vt + 32 * n * L::kValPitch, p[n], lane, o, T{});
-            if (odd) add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, at, key0, b.d, p, limit, lane, o);
             store(t + 1, page1, vis1);
             __syncthreads();
             vis = vis1;
@@ -156,6 +156,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         l = other_half_sum(l);
         int G = a.G;
         asm volatile("" : "+s"(G));   // (what was computed from it before the loop is not kept through it)
+        if (FORM != kPagesInt8)
+            for (int t = max(t0, hidden); t < t1; ++t)
+                if (const uint64_t odd = odd_of[t - hidden] >> key0 & (~0ull >> (64 - 32 * NB)))
+                    add_odd_rows<T, FORM, DB>(a, s, h, odd, t * KEYS + key0, query(G), sq.len - sq.n + row / G, m, hh, o);
         if constexpr (KS > 1) {
             // the second stream's sums to the first: [RG][32] maxima and sums, [RG][32][D + 4]
             float *ml = reinterpret_cast<float *>(smem), *sums = ml + 64 * RG + (group * 32 + l32) * (D + 4) + 4 * hh;

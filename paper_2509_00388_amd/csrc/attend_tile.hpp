@@ -53,6 +53,7 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
     static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 32);
     static constexpr int kDecoded = 16 / kCached * (int)sizeof(T);               // bytes of a piece in the LDS
     static constexpr int kSteps = D * (int)sizeof(T) / 32;                       // matrix steps of a row of keys
+    static constexpr int kWaveRows = 64 / kPieces < 1 ? 1 : 64 / kPieces;        // rows of a wave's turn, next to one another
     static_assert((kSpare || KEYS * kPieces % NT == 0) && NT % kPieces == 0, "whole rows a turn");
 
     // Whether a piece holds an infinity or a NaN.
@@ -79,6 +80,24 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
         return rows;
     }
 
+    // The pieces of a thread: lane j has in `at` the number of the pool's row of the tile's row j.  `together`: the rows of a wave's turn
+    // lie in one page (which holds kWaveRows tokens), so that their place is the same for all lanes and costs scalar instructions only; through
+    // the LDS, which other waves keep busy, the numbers of a tile's rows take several hundred clocks.  offset: the lane's
+    // place within the turn, in bytes.
+    __device__ static __forceinline__ void ask(const void *pages, int at, bool together, int wave_row, int my_row, int row_bytes, uint32_t offset,
+                                               uint4 (&r)[kPer])
+    {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            if (together) {
+                const uint64_t first = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(at, wave_row + u * kRowStep) * (uint32_t)row_bytes;
+                r[u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(pages) + first + offset);
+            } else {
+                const uint64_t row = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (my_row + u * kRowStep), at);
+                r[u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(pages) + row * (uint32_t)row_bytes + offset % (uint32_t)row_bytes);
+            }
+        }
+    }
     // A piece without what is not to be seen.
     __device__ static __forceinline__ uint4 only(const uint4 &v, bool seen)
     {
@@ -194,6 +213,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
             for (int j = 0; j < 4; ++j) {
                 const float4 f = *reinterpret_cast<const float4 *>(ks + 32 * b + 8 * j + 4 * hh);
                 x[b][4 * j] *= f.x; x[b][4 * j + 1] *= f.y; x[b][4 * j + 2] *= f.z; x[b][4 * j + 3] *= f.w;
+                if (j % 2) __builtin_amdgcn_sched_barrier(0);   // (two reads at a time: all of them at once cost 64 registers)
             }
         c = 1.f;
     }
@@ -226,6 +246,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
             p[b][i] = __builtin_amdgcn_exp2f(fmaf(x[b][i], c, -shift));
             l += p[b][i];
         }
+    asm volatile("" : "+v"(l));   // (added up here: put off by the compiler, the sum keeps all weights in registers until later)
 }
 
 // The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
@@ -238,6 +259,7 @@ __device__ __forceinline__ void scale_weights(const float *vs, bool all, uint64_
         for (int j = 0; j < 4; ++j) {
             const float4 f = *reinterpret_cast<const float4 *>(vs + 32 * b + 8 * j + 4 * hh);
             p[b][4 * j] *= f.x; p[b][4 * j + 1] *= f.y; p[b][4 * j + 2] *= f.z; p[b][4 * j + 3] *= f.w;
+            if (j % 2) __builtin_amdgcn_sched_barrier(0);
         }
     if (!all) {
 #pragma unroll
@@ -263,31 +285,39 @@ template <typename T, int FORM> __device__ __forceinline__ float cached_value(co
     }
 }
 
-// What the rows `odd` of a tile, whose values hold infinities or NaN, add to O^T: in the tile's matrix product they would
-// reach the queries that do not see them too (0 x inf), so they went through it as zeros.  Here each of them is a product
-// of its own, which only the lanes that see it keep.  Lane key0 + j has in `at` the number of the pool's row of key j.
-template <typename T, int FORM, int NB, int DB>
-__device__ __forceinline__ void add_odd_rows(const void *Vpages, uint64_t odd, int at, int key0, int d, const float (&p)[NB][16], int limit,
-                                               int lane, f32x16 (&o)[DB])
+// Values with infinities or NaN at positions that only some of a block's queries see: in a tile's matrix product they would
+// reach the others too (0 x inf), so they go through it as zeros, their rows are remembered, and what they add to O^T is
+// added here, behind the tiles, to the queries that see them.  `odd`: rows of the tile that begins at position `first`;
+// q: the lane's query row; m: its maximum.
+template <typename T, int FORM, int DB>
+__device__ __forceinline__ void add_odd_rows(const AttendArgs &a, int s, int h, uint64_t odd, int first, const T *q, int sees, float m,
+                                               int hh, f32x16 (&o)[DB])
 {
-    const int hh = lane >> 5, l32 = lane & 31;
+    constexpr int PER = 16 / (int)sizeof(T);
     for (; odd; odd &= odd - 1) {
-        const int key = __ffsll((unsigned long long)odd) - 1;
-        const long row = __builtin_amdgcn_readlane(at, key0 + key);
-        float w = 0.f;
+        const int pos = first + __ffsll((unsigned long long)odd) - 1;
+        const int page = page_of(a.b, s, pos);
+        if (!q || pos > sees || page < 0) continue;
+        const long row = pool_row(a.b, page, h, pos);
+        float x = 0.f;   // (each half-wave every other piece of the row)
+#pragma unroll 1
+        for (int c = hh * PER; c < a.b.d; c += 2 * PER) {
+            float y[PER];
+            Elem<T>::unpack(*reinterpret_cast<const uint4 *>(q + c), y);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w += 32 * b + acc_row(i, hh) == key ? p[b][i] : 0.f;
-        w = other_half_sum(w);
-#pragma unroll
-        for (int b = 0; b < DB; ++b) {
-            const float v = hh == 0 && 32 * b + l32 < d ? cached_value<T, FORM>(Vpages, row * d + 32 * b + l32) : 0.f;
-            const f32x16 with = __builtin_amdgcn_mfma_f32_32x32x2f32(v, hh == 0 ? w : 0.f, o[b], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[b][i] = key <= limit ? with[i] : o[b][i];
-            __builtin_amdgcn_sched_barrier(0);   // (a block at a time: this is rare, the registers are not its own)
+            for (int e = 0; e < PER; ++e) x = fmaf(y[e], cached_value<T, FORM>(a.Kpages, row * a.b.d + c + e), x);
         }
+        x = other_half_sum(x) * a.c;
+        float w;
+        if constexpr (FORM == kPagesPlain) w = __builtin_amdgcn_exp2f(x - m);
+        else w = __builtin_amdgcn_exp2f(x * a.Kscale[row] - m) * a.Vscale[row];
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = 32 * b + acc_row(i, hh);
+                if (c < a.b.d) o[b][i] = fmaf(w, cached_value<T, FORM>(a.Vpages, row * a.b.d + c), o[b][i]);
+            }
     }
 }
 

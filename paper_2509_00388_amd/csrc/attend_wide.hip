@@ -34,7 +34,7 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
     constexpr int KEYS = 64, NB = 2, DB = D / 32, R = kWideRows;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ uint32_t part[20];
-    __shared__ unsigned long long odd_of[8];   // by tile: its rows that hold infinities or NaN, where not every query sees every key
+    __shared__ unsigned long long odd_of[8];   // of the tiles that some rows do not see all of: values with infinities or NaN
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
     const bool late = wv >= 4;   // half a tile behind (waves w and w + 4 share a SIMD)
     const PagedBatch &b = a.b;
@@ -58,7 +58,9 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
 
     const int pieces = b.d * L::kCached / 16, my_piece = tid % L::kPieces, my_row = tid / L::kPieces;
     const int wave_row = __builtin_amdgcn_readfirstlane(my_row);
-    const int load_piece = min(my_piece, pieces - 1);
+    const int row_bytes = 16 * pieces;
+    const bool together = 1 << b.page_shift >= L::kWaveRows;
+    const uint32_t offset = (uint32_t)((my_row - wave_row) * row_bytes + 16 * min(my_piece, pieces - 1));
     const bool moves = !L::kSpare || wave_row < KEYS;   // (64 bytes a row: half of the waves have no piece of a tile)
     const int to_keys = my_row * L::kKeyPitch + my_piece * L::kDecoded, to_vals = W::kKeys + my_row * L::kValPitch + my_piece * L::kDecoded;
     if (pieces < L::kPieces) {   // columns that d does not reach stay zero
@@ -72,11 +74,14 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
         const int sees = sq.len - sq.n + row / a.G;                                          // last position the lane's row sees
         const int extent = max(0, sq.len - sq.n + (min(row0 + R, rows) - 1) / a.G + 1);      // positions the block sees
         const int first_sees = sq.len - sq.n + row0 / a.G;                                   // last position that all its rows see
+        const int hidden = max(0, first_sees + 1) / KEYS;                                    // the first tile that not all of them see all of
         const int t0 = (int)mp.u0 * pl.step, t1 = min((int)mp.u1 * pl.step, (extent + KEYS - 1) / KEYS);
 
+        auto query = [&](int G) {
+            return row < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / G) * a.q_row + (h * G + row % G) * a.q_head : nullptr;
+        };
         uint4 q[L::kSteps];
-        load_query<T>(row < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + row / a.G) * a.q_row + (h * a.G + row % a.G) * a.q_head : nullptr,
-                      b.d, hh, q);
+        load_query<T>(query(a.G), b.d, hh, q);
         float m = -INFINITY, l = 0.f;
         f32x16 o[DB], x[NB];
         Weights w[NB];
@@ -94,22 +99,18 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
         float scale = 0.f;   // of the key (wave 0) or value (wave 1) `lane`
         auto load = [&](int t, int page) {
             const int at = !is_page(b, page) ? 0 : pool_row(b, page, h, t * KEYS + lane);
-#pragma unroll
-            for (int u = 0; u < L::kPer; ++u) {
-                if (!moves) continue;
-                const long r = __builtin_amdgcn_ds_bpermute(4 * my_row + 4 * u * L::kRowStep, at);   // of lane my_row + u * kRowStep
-                const long piece = r * pieces + load_piece;
-                kr[u] = reinterpret_cast<const uint4 *>(a.Kpages)[piece];
-                vr[u] = reinterpret_cast<const uint4 *>(a.Vpages)[piece];
+            if (moves) {
+                L::ask(a.Kpages, at, together, wave_row, my_row, row_bytes, offset, kr);
+                L::ask(a.Vpages, at, together, wave_row, my_row, row_bytes, offset, vr);
             }
-            if (FORM != kPagesPlain && wv < 2) scale = !is_page(b, page) ? 0.f : wv == 0 ? a.Kscale[at] * a.c : a.Vscale[at];
+            if (FORM != kPagesPlain && wv < 2) scale = (wv == 0 ? a.Kscale : a.Vscale)[at];
         };
         auto store = [&](int t, uint64_t vis) {
             unsigned char *tile = smem + (t % kTiles) * W::kBytes;
             uint64_t odd = 0;
             if (moves && t * KEYS + KEYS - 1 > first_sees) {   // some rows do not see all of it
                 odd = L::odd_rows(vr, wave_row) & vis;
-                if (odd && lane == 0) atomicOr(&odd_of[t % 8], (unsigned long long)odd);
+                if (odd && lane == 0) atomicOr(&odd_of[t - hidden], (unsigned long long)odd);
             }
             if (vis != ~0ull || odd) {   // (places that hold no key of the sequence may hold anything: zeros instead)
                 const uint64_t kseen = vis >> my_row, vseen = (vis & ~odd) >> my_row;
@@ -126,42 +127,50 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
                     L::put(tile + to_vals + u * L::kRowStep * L::kValPitch, vr[u]);
                 }
             }
-            if (FORM != kPagesPlain && wv < 2) reinterpret_cast<float *>(tile + W::kKeys + W::kVals)[64 * wv + lane] = scale;
+            if (FORM != kPagesPlain && wv < 2)   // (a scale without a key may be anything too)
+                reinterpret_cast<float *>(tile + W::kKeys + W::kVals)[64 * wv + lane] = (vis >> lane) & 1 ? (wv == 0 ? scale * a.c : scale) : 0.f;
         };
         // The matrix half: logits of tile `next`, weights of tile `now` times its values, either of them or both.  The operands of
-        // two steps of each are on their way from the LDS while a step is multiplied (left alone, the compiler asks for all of them first
-        // and spills).
+        // AHEAD steps of each are on their way from the LDS while a step is multiplied; nothing may move from step to step (left alone, the
+        // compiler reads an operand right before its product and waits for it, 2200 clocks for 32 products of 32).
         auto products = [&](auto with_values, int now, auto with_logits, int next) {
             constexpr bool PV = decltype(with_values)::value, QK = decltype(with_logits)::value;
-            constexpr int STEPS = D / 8;   // of each: D / 16 steps of two key blocks, four steps of keys for D / 32 blocks of values
+            constexpr int STEPS = D / 8, AHEAD = 3;   // of each: D / 16 steps of two key blocks, four steps of keys for D / 32 blocks of values
             typedef __attribute__((address_space(3))) bf16x4 lds4;
             const unsigned char *kt = smem + (next % kTiles) * W::kBytes + l32 * L::kKeyPitch + 16 * hh;
             const unsigned char *vt = smem + (now % kTiles) * W::kBytes + W::kKeys + (4 * hh + ((lane & 15) >> 2)) * L::kValPitch +
                                       ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+            uint4 kop[AHEAD + 1];
+            bf16x4 lo[AHEAD + 1], hi[AHEAD + 1];
+            auto fetch = [&](int i) {
+                if (QK) kop[i % (AHEAD + 1)] = *reinterpret_cast<const uint4 *>(kt + 32 * (i & 1) * L::kKeyPitch + 32 * (i >> 1));
+                if (PV) {
+                    const int key = 16 * (i / DB), y = i % DB;
+                    lo[i % (AHEAD + 1)] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + key * L::kValPitch + 64 * y));
+                    hi[i % (AHEAD + 1)] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + (key + 8) * L::kValPitch + 64 * y));
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) fetch(i);
             if (QK) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                if (QK) add_block(*reinterpret_cast<const uint4 *>(kt + 32 * (i & 1) * L::kKeyPitch + 32 * (i >> 1)), q[i >> 1], x[i & 1], T{});
+                if (i + AHEAD < STEPS) fetch(i + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                const int at = i % (AHEAD + 1);
+                if (QK) add_block(kop[at], q[i >> 1], x[i & 1], T{});
                 if (PV) {
-                    const int key = 16 * (i / DB), n = key >> 5, st = (key >> 4) & 1, y = i % DB;
-                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + key * L::kValPitch + 64 * y));
-                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + (key + 8) * L::kValPitch + 64 * y));
-                    o[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), w[n].w[st], o[y], 0, 0, 0);
+                    const int n = i / DB >> 1, st = i / DB & 1, y = i % DB;
+                    o[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo[at], hi[at], 0, 1, 2, 3, 4, 5, 6, 7), w[n].w[st], o[y], 0, 0, 0);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            constexpr int reads = (QK ? 1 : 0) + (PV ? 2 : 0), each = (QK ? 1 : 0) + (PV ? 1 : 0), ahead = 2;
-            __builtin_amdgcn_sched_group_barrier(0x100, ahead * reads, 0);   // (LDS reads)
-#pragma unroll
-            for (int i = 0; i < STEPS - ahead; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, each, 0);   // (matrix instructions)
-                __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, ahead * each, 0);
         };
         constexpr std::true_type yes{};
         constexpr std::false_type no{};
@@ -183,29 +192,25 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
             products(no, t0, yes, t0);
             for (int t = t0; t < t1; ++t) {
                 __syncthreads();
-                const uint64_t odd = odd_of[t % 8];
-                if (tid == 0) odd_of[(t + 4) % 8] = 0;   // (last read by the late waves four tiles ago, first written two tiles from now)
                 const uint64_t vis3 = __ballot(is_page(b, page));
                 store(t + 2, vis2);
+                __builtin_amdgcn_sched_barrier(0);
                 load(t + 3, page);
                 page = entry(t + 4);
+                __builtin_amdgcn_sched_barrier(0);
                 const float *ks = reinterpret_cast<const float *>(smem + (t % kTiles) * W::kBytes + W::kKeys + W::kVals);
                 const bool all = vis == ~0ull && t * KEYS + KEYS - 1 <= first_sees;
                 const uint64_t seen = seen_keys(vis, sees - t * KEYS, hh);
                 float p[NB][16];
                 softmax_tile<FORM, NB, DB>(x, ks, a.c, all, seen, hh, m, l, o, p);
                 if constexpr (FORM != kPagesPlain) scale_weights<NB>(ks + KEYS, all, seen, hh, p);
-                if (odd) {
-                    const int again = entry(t);
-                    add_odd_rows<T, FORM, NB, DB>(a.Vpages, odd, !is_page(b, again) ? 0 : pool_row(b, again, h, t * KEYS + lane), 0, b.d, p,
-                                                  sees - t * KEYS, lane, o);
-                }
 #pragma unroll
                 for (int n = 0; n < NB; ++n) w[n] = pack_weights(p[n]);
                 vis = vis1;
                 vis1 = vis2;
                 vis2 = vis3;
                 __syncthreads();
+                __builtin_amdgcn_sched_barrier(0);
                 products(yes, t, yes, t + 1);   // (behind the last tile lies one of zeros: a way out between the two would cost the sums twice the registers)
             }
             if (!late) __builtin_amdgcn_s_barrier();
@@ -214,6 +219,10 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
         l = other_half_sum(l);
         int G = a.G;
         asm volatile("" : "+s"(G));   // (what was computed from it before the loop is not kept through it)
+        if (FORM != kPagesInt8)
+            for (int t = max(t0, hidden); t < t1; ++t)
+                if (const uint64_t odd = odd_of[t - hidden])
+                    add_odd_rows<T, FORM, DB>(a, s, h, odd, t * KEYS, query(G), sq.len - sq.n + row / G, m, hh, o);
         if (tid == 0 && mp.u0 == 0 && mp.u1 < mp.units)
             pl.join.records[me] = {stretch_owner(total, pos + mp.units - 1, n_wg) - me + 1, 2 * me + (pos == mine ? 0 : 1), sq.row0, h, row0,
                                    min(R, rows - row0)};
