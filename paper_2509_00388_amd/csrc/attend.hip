@@ -13,8 +13,6 @@ namespace gkv {
 
 namespace {
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(uint16_t x) { return bf16_to_f32(x); }
 __device__ __forceinline__ void put(float *p, float x) { *p = x; }
 __device__ __forceinline__ void put(uint16_t *p, float x) { *p = (uint16_t)pack_bf16(x, 0.f); }
 
@@ -75,8 +73,8 @@ __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
     if (a.lse && tid == 0) a.lse[(long)row * a.b.H * a.G + hq] = lse_of(m, l);
 }
 
-// The parts of blocks of rows that several workgroups hold, put together: workgroup (w, y) takes rows y * rows_per_wg and on of the
-// block whose first part workgroup w held.  A row is 256 / GROUPS lanes wide, four sums a lane; where the parts are many, several
+// The parts of blocks of rows that several workgroups hold, put together: workgroup (y, w) takes rows y * rows_per_wg and on of the
+// block whose first part workgroup w held (in this order, so that the few w that hold one spread over all XCDs).  A row is 256 / GROUPS lanes wide, four sums a lane; where the parts are many, several
 // groups of lanes share a row's.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan pl)
@@ -84,14 +82,15 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan
     constexpr int LANES = D / 4, GROUPS = 256 / LANES;
     __shared__ float4 sums[GROUPS][LANES];
     __shared__ float totals[GROUPS];
-    const JoinRecord rec = pl.records[blockIdx.x];
-    const int first = blockIdx.y * pl.rows_per_wg, last = min(first + pl.rows_per_wg, rec.rows);
+    const int me = blockIdx.y;
+    const JoinRecord rec = pl.records[me];
+    const int first = blockIdx.x * pl.rows_per_wg, last = min(first + pl.rows_per_wg, rec.rows);
     if (rec.parts == 0 || first >= last) return;
     int share = 1;   // groups a row
-    while (share < GROUPS && (share < rec.parts / 4 || 2 * share * (last - first) <= GROUPS)) share *= 2;
+    while (share < GROUPS && (share < rec.parts / 16 || 2 * share * (last - first) <= GROUPS)) share *= 2;
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, mine = group % share, at_once = GROUPS / share;
     const float *slot0 = pl.slots + (size_t)rec.slot * pl.slot_floats;
-    const float *slots = pl.slots + (size_t)2 * blockIdx.x * pl.slot_floats;   // part k > 0: 2 k slots further
+    const float *slots = pl.slots + (size_t)2 * me * pl.slot_floats;   // part k > 0: 2 k slots further
     for (int r0 = first; r0 < last; r0 += at_once) {
         const int r = min(r0 + group / share, last - 1);
         const int stat = pl.slot_rows * D + 2 * r, at = r * D + 4 * lane;
@@ -145,7 +144,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan
 
 hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &pl, int dtype, hipStream_t st)
 {
-    const dim3 grid(pl.n_wg, (pl.slot_rows + pl.rows_per_wg - 1) / pl.rows_per_wg);
+    const dim3 grid((pl.slot_rows + pl.rows_per_wg - 1) / pl.rows_per_wg, pl.n_wg);
     const int D = attend_width(a.b.d);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
     if (dtype == 0) return D == 64 ? go(attend_join_kernel<float, 64>) : go(attend_join_kernel<float, 128>);

@@ -165,11 +165,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
         l = other_half_sum(l);
         int G = a.G;
         asm volatile("" : "+s"(G));   // (what was computed from it before the loop is not kept through it)
-        if (FORM != kPagesInt8 && (odd_of[0] | odd_of[1]))
-            for (int k = 0; k < 2; ++k)
-                add_odd_rows<T, FORM, DB>(a, s, h, k ? odd_of[1] : odd_of[0], (hidden + k) * pl.tile_keys + wv * KEYS,
-                                          l32 < rows ? reinterpret_cast<const T *>(a.Q) + (sq.row0 + l32 / G) * a.q_row + (h * G + l32 % G) * a.q_head : nullptr,
-                                          sq.len - sq.n + l32 / G, m, hh, o);
         __syncthreads();
         float *ml = reinterpret_cast<float *>(smem), *parts = ml + 256;   // [4][32][2], [4][rows][D + 4]
         if (hh == 0) { ml[(wv * 32 + l32) * 2] = m; ml[(wv * 32 + l32) * 2 + 1] = l; }
@@ -190,6 +185,29 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
                 for (int j = 0; j < 4; ++j)
                     *reinterpret_cast<float4 *>(to + 32 * x + 8 * j) =
                         make_float4(o[x][4 * j] * f, o[x][4 * j + 1] * f, o[x][4 * j + 2] * f, o[x][4 * j + 3] * f);
+        }
+        if (FORM != kPagesInt8 && (odd_of[0] | odd_of[1])) {
+            // Values with infinities or NaN at positions that only some rows see went through the products as zeros (0 x inf would reach
+            // the other rows too): what they add to the rows that see them is added here.
+            wave_sync();
+            for (int k = 0; k < 2; ++k)
+                for (uint64_t odd = k ? odd_of[1] : odd_of[0]; odd; odd &= odd - 1) {
+                    const int at_pos = (hidden + k) * pl.tile_keys + wv * KEYS + __ffsll((unsigned long long)odd) - 1;
+                    const int at_page = page_of(b, s, at_pos);
+                    if (at_page < 0) continue;
+                    const long row = pool_row(b, at_page, h, at_pos);
+                    for (int r = max(0, at_pos - (sq.len - sq.n)) * G; r < rows; ++r) {   // the rows from that position on
+                        const T *qr = reinterpret_cast<const T *>(a.Q) + (sq.row0 + r / G) * a.q_row + (h * G + r % G) * a.q_head;
+                        float x = 0.f;
+                        for (int c = lane; c < b.d; c += kWave) x = fmaf(to_float(qr[c]), cached_value<T, FORM>(a.Kpages, row * b.d + c), x);
+                        x = wave_sum(x) * a.c;
+                        if (FORM != kPagesPlain) x *= a.Kscale[row];
+                        float w = __builtin_amdgcn_exp2f(x - __shfl(shift, r, kWave));
+                        if (FORM != kPagesPlain) w *= a.Vscale[row];
+                        for (int c = lane; c < b.d; c += kWave)
+                            parts[(wv * rows + r) * (D + 4) + c] += w * cached_value<T, FORM>(a.Vpages, row * b.d + c);
+                    }
+                }
         }
         const bool whole = t0 == 0 && t1 == (int)per_head;
         const int slot_at = 2 * blockIdx.x + (tile == mine ? 0 : 1);

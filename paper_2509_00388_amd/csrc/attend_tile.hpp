@@ -111,6 +111,19 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
         if constexpr (FORM == kPagesPlain) {
             w[0] = v;
         } else {
+            if constexpr (FORM == kPagesFp8 && sizeof(T) == 2) {   // (two codes an instruction, the scale 1)
+                typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                const uint32_t c[4] = {v.x, v.y, v.z, v.w};
+                union { bf16x2 b[8]; uint4 u[2]; } y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y.b[2 * e] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.f, false);
+                    y.b[2 * e + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.f, true);
+                }
+                w[0] = y.u[0];
+                w[1] = y.u[1];
+                return;
+            }
             float x[16];
             Cached<T, FORM>::unpack(v, x);
             if constexpr (sizeof(T) == 4) {
@@ -268,6 +281,9 @@ __device__ __forceinline__ void scale_weights(const float *vs, bool all, uint64_
             for (int i = 0; i < 16; ++i) p[b][i] = (seen >> (32 * b + acc_row(i, 0))) & 1 ? p[b][i] : 0.f;
     }
 }
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return bf16_to_f32(x); }
 
 // A value of a cached row.
 template <typename T, int FORM> __device__ __forceinline__ float cached_value(const void *rows, long at)
