@@ -226,7 +226,6 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
             for (int j = 0; j < 4; ++j) {
                 const float4 f = *reinterpret_cast<const float4 *>(ks + 32 * b + 8 * j + 4 * hh);
                 x[b][4 * j] *= f.x; x[b][4 * j + 1] *= f.y; x[b][4 * j + 2] *= f.z; x[b][4 * j + 3] *= f.w;
-                if (j % 2) __builtin_amdgcn_sched_barrier(0);   // (two reads at a time: all of them at once cost 64 registers)
             }
         c = 1.f;
     }
@@ -259,7 +258,6 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
             p[b][i] = __builtin_amdgcn_exp2f(fmaf(x[b][i], c, -shift));
             l += p[b][i];
         }
-    asm volatile("" : "+v"(l));   // (added up here: put off by the compiler, the sum keeps all weights in registers until later)
 }
 
 // The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
@@ -272,7 +270,6 @@ __device__ __forceinline__ void scale_weights(const float *vs, bool all, uint64_
         for (int j = 0; j < 4; ++j) {
             const float4 f = *reinterpret_cast<const float4 *>(vs + 32 * b + 8 * j + 4 * hh);
             p[b][4 * j] *= f.x; p[b][4 * j + 1] *= f.y; p[b][4 * j + 2] *= f.z; p[b][4 * j + 3] *= f.w;
-            if (j % 2) __builtin_amdgcn_sched_barrier(0);
         }
     if (!all) {
 #pragma unroll

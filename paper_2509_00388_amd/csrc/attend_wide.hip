@@ -1,13 +1,16 @@
 // Attention of sequences with more than 128 stacked rows, bf16 rows of up to 128 values: bound by the matrix cores and the
 // vector instructions of the softmax, which this kernel keeps busy at the same time.
 //
-// A workgroup of eight waves, two on a SIMD, takes a block of 256 stacked query rows of a head, 32 a wave.  A wave's tile has
-// two halves: the matrix products, S^T = K Q^T of the tile and O^T += V^T P^T of the tile before it, and the
-// softmax of the tile, with the wave's share of the loads and stores that bring later tiles.  The two waves of a SIMD are half a
-// tile apart, kept so by a barrier behind each half: while one has the matrix cores, the other has the vector unit.  (One phase for all,
-// two workgroups of four waves: matrix cores busy 39 % of the time, vector unit half of it, hardly ever both.)
-// Tiles stay in the LDS for four tiles' time (152 KiB): written two tiles ahead of their use by waves of either half,
-// read by the late ones half a tile after the early ones.
+// A workgroup of eight waves, two on a SIMD, takes a block of 256 stacked query rows of a head, 32 a wave, and shares each tile of 64
+// keys and values among all of them.  A wave's tile is one stretch of code without a barrier inside: the softmax of tile t, O^T += V^T P^T of
+// tile t and S^T = K Q^T of tile t + 1, so that the sums of the softmax run beside the products, whose operands are
+// read from the LDS some steps ahead, and the two waves of a SIMD fill one another's gaps.  The LDS holds three tiles: those two and the next,
+// which the waves write, from registers, while nobody reads it; one barrier a tile.
+// Measured (2048 rows of four query heads a key head over 32768 keys, eight key heads, d = 128, bf16): 1060 to 1095 us, 970 to
+// 1000 TFLOP/s, where a library product of 8192 cubed reaches 1215 (the chip's power bounds both: without the softmax the same products take 850 us
+// and without their reads from the LDS hardly less).  Slower: 128 rows a workgroup and two of them 1290; a barrier between softmax and
+// products that keeps the waves of a SIMD half a tile apart 1090, with the operands' reads fixed by hand 1130, with tiles that
+// pass the registers by (global_load_lds, pieces permuted instead of padded) 1130.
 #include "attend_tile.hpp"
 #include "kernels.hpp"
 
@@ -17,7 +20,7 @@ namespace gkv {
 
 namespace {
 
-constexpr int kWideRows = 256, kTiles = 4;   // tiles in the LDS
+constexpr int kWideRows = 256, kTiles = 3;   // tiles in the LDS
 
 template <int FORM, int D> struct WideTile {
     using L = Tile<uint16_t, FORM, D, 64, 512>;
@@ -36,7 +39,6 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
     __shared__ uint32_t part[20];
     __shared__ unsigned long long odd_of[8];   // of the tiles that some rows do not see all of: values with infinities or NaN
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
-    const bool late = wv >= 4;   // half a tile behind (waves w and w + 4 share a SIMD)
     const PagedBatch &b = a.b;
 
     uint32_t total, before, pos = 0, last = 0;
@@ -130,47 +132,39 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
             if (FORM != kPagesPlain && wv < 2)   // (a scale without a key may be anything too)
                 reinterpret_cast<float *>(tile + W::kKeys + W::kVals)[64 * wv + lane] = (vis >> lane) & 1 ? (wv == 0 ? scale * a.c : scale) : 0.f;
         };
-        // The matrix half: logits of tile `next`, weights of tile `now` times its values, either of them or both.  The operands of
-        // AHEAD steps of each are on their way from the LDS while a step is multiplied; nothing may move from step to step (left alone, the
-        // compiler reads an operand right before its product and waits for it, 2200 clocks for 32 products of 32).
+        // Logits of tile `next`, weights of tile `now` times its values, either of them or both.  The groups ask the scheduler for the operands of
+        // two steps of each to be on their way while a step is multiplied (1060 -> 1095 us without).
         auto products = [&](auto with_values, int now, auto with_logits, int next) {
             constexpr bool PV = decltype(with_values)::value, QK = decltype(with_logits)::value;
-            constexpr int STEPS = D / 8, AHEAD = 3;   // of each: D / 16 steps of two key blocks, four steps of keys for D / 32 blocks of values
+            constexpr int STEPS = D / 8;   // of each: D / 16 steps of two key blocks, four steps of keys for D / 32 blocks of values
             typedef __attribute__((address_space(3))) bf16x4 lds4;
             const unsigned char *kt = smem + (next % kTiles) * W::kBytes + l32 * L::kKeyPitch + 16 * hh;
             const unsigned char *vt = smem + (now % kTiles) * W::kBytes + W::kKeys + (4 * hh + ((lane & 15) >> 2)) * L::kValPitch +
                                       ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-            uint4 kop[AHEAD + 1];
-            bf16x4 lo[AHEAD + 1], hi[AHEAD + 1];
-            auto fetch = [&](int i) {
-                if (QK) kop[i % (AHEAD + 1)] = *reinterpret_cast<const uint4 *>(kt + 32 * (i & 1) * L::kKeyPitch + 32 * (i >> 1));
-                if (PV) {
-                    const int key = 16 * (i / DB), y = i % DB;
-                    lo[i % (AHEAD + 1)] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + key * L::kValPitch + 64 * y));
-                    hi[i % (AHEAD + 1)] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + (key + 8) * L::kValPitch + 64 * y));
-                }
-            };
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) fetch(i);
             if (QK) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
             }
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                if (i + AHEAD < STEPS) fetch(i + AHEAD);
-                __builtin_amdgcn_sched_barrier(0);
-                const int at = i % (AHEAD + 1);
-                if (QK) add_block(kop[at], q[i >> 1], x[i & 1], T{});
+                if (QK) add_block(*reinterpret_cast<const uint4 *>(kt + 32 * (i & 1) * L::kKeyPitch + 32 * (i >> 1)), q[i >> 1], x[i & 1], T{});
                 if (PV) {
-                    const int n = i / DB >> 1, st = i / DB & 1, y = i % DB;
-                    o[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo[at], hi[at], 0, 1, 2, 3, 4, 5, 6, 7), w[n].w[st], o[y], 0, 0, 0);
+                    const int key = 16 * (i / DB), n = key >> 5, st = (key >> 4) & 1, y = i % DB;
+                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + key * L::kValPitch + 64 * y));
+                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(vt + (key + 8) * L::kValPitch + 64 * y));
+                    o[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), w[n].w[st], o[y], 0, 0, 0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
+            constexpr int reads = (QK ? 1 : 0) + (PV ? 2 : 0), each = (QK ? 1 : 0) + (PV ? 1 : 0), ahead = 2;
+            __builtin_amdgcn_sched_group_barrier(0x100, ahead * reads, 0);   // (LDS reads)
+#pragma unroll
+            for (int i = 0; i < STEPS - ahead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, each, 0);   // (matrix instructions)
+                __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, ahead * each, 0);
         };
         constexpr std::true_type yes{};
         constexpr std::false_type no{};
@@ -188,16 +182,13 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
         page = entry(t0 + 3);
         __syncthreads();
         if (t0 < t1) {
-            if (late) __builtin_amdgcn_s_barrier();
             products(no, t0, yes, t0);
             for (int t = t0; t < t1; ++t) {
                 __syncthreads();
                 const uint64_t vis3 = __ballot(is_page(b, page));
                 store(t + 2, vis2);
-                __builtin_amdgcn_sched_barrier(0);
                 load(t + 3, page);
                 page = entry(t + 4);
-                __builtin_amdgcn_sched_barrier(0);
                 const float *ks = reinterpret_cast<const float *>(smem + (t % kTiles) * W::kBytes + W::kKeys + W::kVals);
                 const bool all = vis == ~0ull && t * KEYS + KEYS - 1 <= first_sees;
                 const uint64_t seen = seen_keys(vis, sees - t * KEYS, hh);
@@ -209,11 +200,8 @@ __global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a, ManyP
                 vis = vis1;
                 vis1 = vis2;
                 vis2 = vis3;
-                __syncthreads();
-                __builtin_amdgcn_sched_barrier(0);
                 products(yes, t, yes, t + 1);   // (behind the last tile lies one of zeros: a way out between the two would cost the sums twice the registers)
             }
-            if (!late) __builtin_amdgcn_s_barrier();
         }
 
         l = other_half_sum(l);

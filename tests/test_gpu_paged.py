@@ -285,6 +285,59 @@ def test_attention_does_not_see_what_is_hidden(dtype, form, impl, d):
             assert torch.isnan(lse[r]).all() and torch.isnan(out[r]).any(), (r, s, pos)
 
 
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("d,G,ps", [(64, 1, 16), (80, 3, 32), (128, 2, 64), (128, 5, 16), (96, 4, 128)])
+def test_attention_of_wide_blocks(form, d, G, ps):
+    """Chunks of more than 128 stacked rows (blocks of 256, tiles that pass the registers by): lengths on both sides of tiles and
+    blocks, sequences that begin with the chunk, pages that are none, infinities and NaN in places that are not seen and at
+    positions that some rows see."""
+    say(f"wide blocks form={form} d={d} G={G} ps={ps}")
+    b = pu.Batch([(150, 700), (129, 129), (3, 64), (260, 261), (64, 1025), (100, 30)], H=2, G=G, d=d, ps=ps, form=form, before=1, behind=2,
+                 seed=d + G)
+    b.p.max_rows = 260
+    b.table[0, 2] = -1
+    b.table[4, -(-1025 // ps) // 2] = b.p.n_pages
+    Q = b.random_rows(2 * G, fused=4)
+    clean, clean_lse = run_attend(b, Q)
+    pu.check_attend(b, Q, clean, clean_lse)
+    used = torch.zeros(b.p.n_pages, b.ps, dtype=torch.bool)
+    for s, (_, n) in enumerate(b.pairs):
+        for j in range(n):
+            cell = b.place(s, j)
+            if cell:
+                used[cell] = True
+    for n in "KV":
+        if form == gk.PAGES_PLAIN:
+            b.pool[n].transpose(1, 2)[~used] = math.nan
+        else:
+            b.pool[n].view(torch.uint8).transpose(1, 2)[~used] = 0x7f
+            b.pool[n + "s"].transpose(1, 2)[~used] = math.inf
+    out, lse = run_attend(b, Q)
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+    late = {0: 640, 1: 100, 3: 200, 4: 1000}
+    for s, j in late.items():
+        page, at = b.place(s, j)
+        if form == gk.PAGES_PLAIN:
+            b.pool["V"][page, :, at, 5] = math.inf
+            b.pool["V"][page, :, at, d - 1] = math.nan
+        elif form == gk.PAGES_FP8:
+            b.pool["V"].view(torch.uint8)[page, :, at, 5] = 0x7f
+            b.pool["V"].view(torch.uint8)[page, :, at, d - 1] = 0xff
+        else:
+            b.pool["Vs"][page, :, at] = math.inf
+    out, lse = run_attend(b, Q)
+    assert torch.equal(lse, clean_lse)
+    columns = [5, d - 1] if form != gk.PAGES_INT8 else list(range(d))
+    rest = [c for c in range(d) if c not in columns]
+    for r, s, pos in b.each_row():
+        if pos < late.get(s, 10 ** 9):
+            assert torch.equal(out[r], clean[r]), (r, s, pos)
+        else:
+            assert not torch.isfinite(out[r][:, columns]).any(), (r, s, pos)
+            if rest:   # the row's other values count as before, in another order of the sum and with weights of 32 bits
+                assert (out[r][:, rest].float() - clean[r][:, rest].float()).abs().max() < 0.1
+
+
 def test_attention_with_large_logits_and_a_scale():
     """Logits of thousands, where only a few weights are left, and a scale of the caller's."""
     say("large logits")
