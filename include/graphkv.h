@@ -281,7 +281,8 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
  *             tokens.  With n of them, row row_start[s] + i has position
  *             seq_len[s] - n + i.
  * table, seq_len and row_start are DEVICE arrays, read when the kernels run: a captured
- * graph serves batches whose lengths change from replay to replay.  Rows before
+ * graph serves batches whose lengths change from replay to replay (make the first call
+ * with a set of params outside a capture: it opts kernels in to large shared memory).  Rows before
  * row_start[0] and from row_start[n_seqs] on belong to no sequence: none of their
  * outputs is written (a batch padded to a fixed number of rows).
  *
@@ -346,7 +347,8 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  *   out = sum_j softmax_j(<q, k_j> * scale) v_j,   lse = log sum_j exp(<q, k_j> * scale),
  * with query head i on key-value head i / (H_q / H_kv).  One token a sequence, a few
  * drafted ones, a chunk of a prompt, or a mixture of these in one call.
- *   Q    [n_rows, H_q, d] in, out [n_rows, H_q, d] out, with their strides
+ *   Q    [n_rows, H_q, d] in, out [n_rows, H_q, d] out, with their strides; they must not
+ *        overlap
  *   lse  [n_rows, H_q]    out, optional (NULL), fp32
  *   ws   graphkv_attend_workspace_bytes(p) bytes, 256-byte aligned
  * Softmax statistics and sums are held in 32 bits; with bf16 rows the weights are

@@ -373,9 +373,13 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
     if (((tokens + 127) / 128) * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
     if ((int64_t)p->n_rows * A.G > (1 << 30)) return false;   // (and so are stacked rows)
-    // Sequences of few rows and of many are different kernels' where both can occur; a batch of one sequence is one or the other.
+    // Sequences of few rows and of many go to different kernels where there are enough of both for two more launches: from eight
+    // sequences on, unless the rows are as many as if all of them were as long as they may be (which the device alone knows: either
+    // kernel for many rows takes any).  (A chunk of 500 rows beside steps over 2000 to 5000 tokens, eight key heads of four, us for one kernel
+    // / for both: plain pages, 3 steps 102 / 107, 7 106 / 113, 23 185 / 168, 127 561 / 436; fp8 pages 115 / 116, 124 / 115, 211 / 149,
+    // 690 / 304.  16 sequences of 64 rows each: 116 / 122.)
     A.many = (int64_t)b.max_rows * A.G > kFewRows;
-    A.few = !A.many || b.n_seqs > 1;
+    A.few = !A.many || (b.n_seqs >= 8 && (int64_t)b.n_seqs * b.max_rows > b.n_rows);
     if (A.few) {
         A.fp = few_plan(b, p->dtype, p->page_format, A.G);
         A.few_slots = align_up(join_record_bytes(A.fp.join));
@@ -383,6 +387,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     }
     if (A.many) {
         A.mp = many_plan(b, p->dtype, A.G, A.few);
+        if (A.mp.join.n_wg == 0) return false;
         A.many_records = A.total;
         A.many_slots = A.many_records + align_up(join_record_bytes(A.mp.join));
         A.total = A.many_slots + align_up(join_slot_bytes(A.mp.join));

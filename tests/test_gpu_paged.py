@@ -192,6 +192,11 @@ SHAPES = [
     dict(pairs=[(100, 300)], H=2, G=4, d=128), dict(pairs=[(33, 33)], H=3, G=1, d=64, ps=32),
     dict(pairs=[(1, 150), (70, 200), (8, 90), (129, 130)], H=2, G=2, d=128, ps=32),
     dict(pairs=[(19, 260), (0, 50), (50, 50)], H=2, G=7, d=96, ps=128),
+    # many sequences of either kind: both kernels
+    dict(pairs=[(1, 150), (70, 200), (8, 90), (129, 130), (1, 1), (1, 33), (2, 64), (0, 9), (1, 400)], H=2, G=2, d=128, ps=32),
+    dict(pairs=[(1, 90), (30, 60), (2, 90), (1, 0), (1, 7), (1, 33), (5, 64), (3, 2), (40, 100)], H=2, G=7, d=64, ps=2),
+    # a token a page, blocks of each size
+    dict(pairs=[(150, 200)], H=1, G=2, d=128, ps=1), dict(pairs=[(60, 130)], H=1, G=1, d=80, ps=2), dict(pairs=[(100, 101)], H=2, G=1, d=128, ps=4),
     # other head dimensions
     dict(pairs=[(1, 200), (40, 140)], H=2, G=2, d=256), dict(pairs=[(3, 120)], H=2, G=2, d=160, ps=64),
     dict(pairs=[(2, 90), (20, 60)], H=1, G=2, d=512), dict(pairs=[(1, 100), (45, 45)], H=2, G=1, d=16),
@@ -360,3 +365,167 @@ def test_attention_of_many_sequences(dtype):
     Q = b.random_rows(2)
     out, lse = run_attend(b, Q)
     pu.check_attend(b, Q, out, lse)
+
+
+# ---- together, in graphs, on streams ----------------------------------------------------------------
+
+def test_prefill_evict_decode():
+    """The calls as a serving loop makes them: chunks of a prompt written and attended over, the prompt read back and evicted, what
+    is kept written to fewer pages, tokens generated behind it."""
+    say("prefill, evict, decode")
+    H, G, d, ps, N, w, B = 2, 4, 128, 32, 700, 16, 150
+    g = torch.Generator("cuda").manual_seed(3)
+    for form in FORMS:
+        pool = [torch.zeros(40, H, ps, d, device="cuda").to(pu.CODE.get(form, torch.bfloat16)) for _ in range(2)]
+        scales = [] if form == gk.PAGES_PLAIN else [torch.zeros(40, H, ps, device="cuda") for _ in range(2)]
+        qkv = torch.randn(N, (G + 2) * H, d, generator=g, device="cuda").to(torch.bfloat16)
+        Q, K, V = qkv[:, :G * H], qkv[:, G * H:G * H + H], qkv[:, G * H + H:]
+        table = torch.randperm(40, generator=g, device="cuda").to(torch.int32)[None, :24].contiguous()
+        p = gk.PagedParams(n_kv_heads=H, n_q_heads=G * H, head_dim=d, page_tokens=ps, n_pages=40, n_seqs=1, table_pages=24, n_rows=0,
+                           page_format=form)
+        i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+        out = torch.empty(N, G * H, d, dtype=torch.bfloat16, device="cuda")
+        for a, e in ((0, 1), (1, 300), (300, 311), (311, N)):
+            p.n_rows = e - a
+            batch = (table, i32(e), i32(0, e - a))
+            gk.graphkv_cache_write(p, K[a:e], V[a:e], *pool, *batch, *scales)
+            gk.graphkv_attend(p, Q[a:e], *pool, *batch, *scales, out=out[a:e])
+        # the whole prompt again as one batch of rows, [H, N, d] as the eviction pass takes it
+        p.n_rows = N
+        batch = (table, i32(N), i32(0, N))
+        Kc, Vc = (torch.empty(H, N, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        gk.graphkv_cache_read(p, *pool, *batch, *scales, K=Kc.transpose(0, 1), V=Vc.transpose(0, 1))
+        if form == gk.PAGES_PLAIN:
+            assert torch.equal(Kc, K.transpose(0, 1)) and torch.equal(Vc, V.transpose(0, 1))
+        hidden = torch.ones(N, N, dtype=torch.bool, device="cuda").triu(1)
+        k, v = (t.double().repeat_interleave(G, 0) for t in (Kc, Vc))
+        x = (Q.transpose(0, 1).double().contiguous() @ k.transpose(1, 2).contiguous() / math.sqrt(d)).masked_fill(hidden, -math.inf)
+        want = (torch.softmax(x, -1) @ v).transpose(0, 1)
+        # weights of bf16, and for coded pages values that were rounded to bf16 on their way back, as the keys were
+        allow = 2 * pu.half_step(torch.bfloat16) * (torch.softmax(x, -1) @ v.abs()).transpose(0, 1) + pu.half_step(torch.bfloat16) * want.abs()
+        if form != gk.PAGES_PLAIN:
+            shift = pu.half_step(torch.bfloat16) * (Q.transpose(0, 1).double().abs().contiguous() @ k.abs().transpose(1, 2).contiguous()).amax(-1) / math.sqrt(d)
+            allow = allow + (2 * shift.T[..., None] + pu.half_step(torch.bfloat16)) * (torch.softmax(x, -1) @ v.abs()).transpose(0, 1)
+        assert ((out.double() - want).abs() <= allow + 1e-4).all()
+        # eviction, the kept rows to five other pages
+        ep = gk.Params(n_kv_heads=H, n_q_heads=G * H, head_dim=d, n_tokens=N, window=w, pool_kernel=5, budget=B, n_sources=8, n_neighbors=4, rounds=1)
+        Ko, Vo, idx = gk.graphkv_compress(ep, Kc, Vc, Q[N - w:].transpose(0, 1).contiguous())
+        kept = torch.arange(30, 35, device="cuda", dtype=torch.int32)[None].contiguous()
+        kp = gk.PagedParams(n_kv_heads=H, n_q_heads=G * H, head_dim=d, page_tokens=ps, n_pages=40, n_seqs=1, table_pages=5, n_rows=B, page_format=form)
+        gk.graphkv_cache_write(kp, Ko.transpose(0, 1), Vo.transpose(0, 1), *pool, kept, i32(B), i32(0, B), *scales)
+        kp.n_rows = 1
+        for step in range(3):
+            new = torch.randn(1, (G + 2) * H, d, generator=g, device="cuda").to(torch.bfloat16)
+            batch = (kept, i32(B + 1 + step), i32(0, 1))
+            gk.graphkv_cache_write(kp, new[:, G * H:G * H + H], new[:, G * H + H:], *pool, *batch, *scales)
+            got = gk.graphkv_attend(kp, new[:, :G * H], *pool, *batch, *scales)
+            b = pu.Batch([(1, B + 1 + step)], H=H, G=G, d=d, ps=ps, form=form)
+            b.p, b.table = kp, kept.cpu()
+            b.pool = {n: t.cpu() for n, t in zip(("K", "V", "Ks", "Vs"), pool + scales)}
+            pu.check_attend(b, new[:, :G * H].cpu(), got)
+
+
+@pytest.mark.parametrize("pairs,d,form", [([(1, 60)] * 3 + [(1, 900)], 128, gk.PAGES_PLAIN), ([(8, 200), (1, 40), (100, 150)], 128, gk.PAGES_FP8),
+                                          ([(40, 90)], 64, gk.PAGES_INT8)])
+def test_captured_calls_follow_the_lengths(pairs, d, form):
+    """A captured write and attention, replayed with other rows, lengths and pages, with eager work between: the eager calls' bits."""
+    say(f"captured calls {pairs} d={d} form={form}")
+    b = pu.Batch(pairs, H=2, G=4, d=d, ps=16, form=form, behind=3, table_pages=80, spare=80 * len(pairs))
+    # (every page once, whatever the lengths: no two rows of a write may have the same place)
+    b.table = torch.randperm(b.p.n_pages, generator=b.g)[:80 * len(pairs)].reshape(-1, 80).int()
+    K, V, Q = (on_gpu(b.random_rows(h)) for h in (2, 2, 8))
+    args = b.device()
+    ws = gk.alloc_attend_workspace(b.p)
+    out, lse = torch.zeros(b.rows, 8, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(b.rows, 8, device="cuda")
+
+    def step(o, le, w):
+        gk.graphkv_cache_write(b.p, K, V, *args)
+        gk.graphkv_attend(b.p, Q, *args, out=o, lse=le, ws=w)
+
+    step(out, lse, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, lse, ws)
+    g = torch.Generator("cuda").manual_seed(1)
+    for n in range(4):
+        for t in (K, V, Q):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        lens = torch.tensor([min(m + 37 * n, 1200) for _, m in pairs], dtype=torch.int32)
+        if n == 2:
+            lens[0] = 0
+        args[3].copy_(lens)
+        args[2].copy_(args[2].roll(n, 1))
+        pools = [t.clone() for t in args[:2] + args[5:]]
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse, got_pools = out.clone(), lse.clone(), [t.clone() for t in args[:2] + args[5:]]
+        for t, was in zip(args[:2] + args[5:], pools):
+            t.copy_(was)
+        want, want_lse = torch.zeros_like(out), torch.zeros_like(lse)
+        step(want, want_lse, torch.randint(0, 256, ws.shape, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(got_lse, want_lse), f"replay {n}"
+        for x, y in zip(got_pools, args[:2] + args[5:]):
+            assert torch.equal(bits(x), bits(y))
+
+
+def test_two_streams_with_a_workspace_each():
+    say("two streams")
+    sets = []
+    for seed, pairs in ((1, [(1, 3000)]), (2, [(60, 500), (1, 700)])):
+        b = pu.Batch(pairs, H=2, G=4, d=128, ps=16, seed=seed)
+        Q = on_gpu(b.random_rows(8))
+        args = b.device()
+        sets.append((b, Q, args, gk.alloc_attend_workspace(b.p), gk.graphkv_attend(b.p, Q, *args), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(5):
+        for b, Q, args, ws, want, stream in sets:
+            with torch.cuda.stream(stream):
+                outs.append((gk.graphkv_attend(b.p, Q, *args, ws=ws), want))
+    torch.cuda.synchronize()
+    for got, want in outs:
+        assert torch.equal(got, want)
+
+
+def test_strided_outputs_leave_the_rest_alone():
+    say("strided outputs")
+    b = pu.Batch([(3, 40), (50, 90)], H=2, G=2, d=64, ps=16)
+    Q, args = on_gpu(b.random_rows(4)), b.device()
+    want = gk.graphkv_attend(b.p, Q, *args)
+    wide = torch.full((b.rows, 6, 96), -7.0, dtype=torch.bfloat16, device="cuda")
+    gk.graphkv_attend(b.p, Q, *args, out=wide[:, 1:5, 16:80])
+    assert torch.equal(wide[:, 1:5, 16:80], want)
+    wide[:, 1:5, 16:80] = -7
+    assert (wide == -7).all()
+    by_head = torch.empty(4, b.rows, 64, dtype=torch.bfloat16, device="cuda")
+    gk.graphkv_attend(b.p, Q, *args, out=by_head.transpose(0, 1))
+    assert torch.equal(by_head.transpose(0, 1), want)
+
+
+def test_binding_refuses_wrong_tensors():
+    say("wrong tensors")
+    b = pu.Batch([(3, 40)], H=2, G=2, d=64, ps=16, form=gk.PAGES_INT8)
+    Q, args = on_gpu(b.random_rows(4)), b.device()
+    K = on_gpu(b.random_rows(2))
+    good = lambda: list(args)
+
+    def refuse(match, f, *a, **kw):
+        with pytest.raises(gk.GraphKVError, match=match):
+            f(b.p, *a, **kw)
+
+    for i, bad in ((0, args[0].to(torch.uint8)), (0, args[0][:-1]), (1, args[1].transpose(0, 1)), (2, args[2].long()), (3, args[3][:0]),
+                   (4, args[4].cpu()), (5, args[5].double()), (6, None)):
+        a = good()
+        a[i] = bad
+        refuse(".", gk.graphkv_attend, Q, *a)
+    refuse("shape", gk.graphkv_attend, Q[:-1], *args)
+    refuse("dtype", gk.graphkv_attend, Q.float(), *args)
+    refuse("strides", gk.graphkv_attend, Q.expand(3, 4, 64)[:1].expand(3, 4, 64), *args)
+    refuse("strides", gk.graphkv_attend, torch.empty(3, 4, 128, dtype=torch.bfloat16, device="cuda")[..., ::2], *args)
+    refuse("same strides", gk.graphkv_cache_write, K, on_gpu(b.random_rows(2, by_head=True)), *args)
+    refuse("lse", gk.graphkv_attend, Q, *args, lse=torch.empty(3, 3, device="cuda"))
+    refuse("-2", gk.graphkv_attend, Q, *args, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    refuse("-1", gk.graphkv_attend, Q, *args, out=torch.empty(400, dtype=torch.bfloat16, device="cuda").as_strided((3, 4, 64), (64, 64, 1)))
+    torch.cuda.synchronize()
