@@ -310,14 +310,14 @@ typedef struct graphkv_paged_params {
     int32_t n_pages;       /* n_pages * H_kv * page_tokens < 2^31                        */
     int32_t n_seqs;        /* 0 .. 2^20                                                  */
     int32_t table_pages;   /* >= 1, table_pages * page_tokens <= 2^30                    */
-    int32_t n_rows;        /* rows of the row tensors, 0 .. 2^26                         */
+    int32_t n_rows;        /* rows of the row tensors, 0 .. 2^24 - 1                     */
     int32_t max_rows;      /* no sequence has more rows than this; 0: n_rows             */
-    float   softmax_scale; /* attend: 0 selects 1/sqrt(d)                                */
+    float   softmax_scale; /* attend: 0 selects 1/sqrt(d), else in (0, 2^127]            */
     int32_t impl;          /* GRAPHKV_IMPL_*: GENERIC forces the scalar kernel (attend)  */
     int64_t row_stride;    /* elements between rows and between heads of K and V (write, */
     int64_t head_stride;   /*   read) or Q (attend); both 0: packed [n_rows, heads, d].  */
     int64_t out_row_stride;   /* the same for the output of attend.  Strides are         */
-    int64_t out_head_stride;  /*   multiples of 16 bytes; outputs must not overlap       */
+    int64_t out_head_stride;  /*   multiples of 16 bytes, <= 2^38; output rows must not overlap */
 } graphkv_paged_params;
 
 /*

@@ -304,7 +304,8 @@ bool paged_ok(const graphkv_paged_params *p)
     if (p->n_pages < 1 || (__int128)p->n_pages * p->n_kv_heads * p->page_tokens > INT32_MAX) return false;
     if (p->n_seqs < 0 || p->n_seqs > (1 << 20)) return false;
     if (p->table_pages < 1 || (int64_t)p->table_pages * p->page_tokens > (1 << 30)) return false;
-    if (p->n_rows < 0 || p->n_rows > (1 << 26) || p->max_rows < 0 || p->max_rows > p->n_rows) return false;
+    // (a launch has at most 2^32 - 1 threads a dimension, and the scalar kernel 256 a row)
+    if (p->n_rows < 0 || p->n_rows >= (1 << 24) || p->max_rows < 0 || p->max_rows > p->n_rows) return false;
     if (p->impl != GRAPHKV_IMPL_AUTO && p->impl != GRAPHKV_IMPL_GENERIC) return false;
     return true;
 }
@@ -312,7 +313,7 @@ bool paged_ok(const graphkv_paged_params *p)
 // Strides of a tensor [n_rows, heads, d]; both 0: packed.  `distinct`: no two of its rows may overlap.
 bool take_strides(const graphkv_paged_params *p, int heads, int64_t row_stride, int64_t head_stride, bool distinct, long &row, long &head)
 {
-    const int64_t d = p->head_dim, unit = p->dtype == GRAPHKV_FP32 ? 4 : 8, most = (int64_t)1 << 44;
+    const int64_t d = p->head_dim, unit = p->dtype == GRAPHKV_FP32 ? 4 : 8, most = (int64_t)1 << 38;   // (times n_rows in 64 bits)
     row = row_stride;
     head = head_stride;
     if (row == 0 && head == 0) {
@@ -350,6 +351,8 @@ bool batch_pointers_ok(const graphkv_paged_params *p, const void *Kpages, const 
            aligned(table, 4) && aligned(seq_len, 4) && aligned(row_start, 4);
 }
 
+constexpr float kLog2e = 1.4426950408889634f;   // (logits are taken to base 2)
+
 // Which kernels graphkv_attend launches, and what they leave in its workspace.
 struct AttendPlan {
     int G;
@@ -363,7 +366,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
 {
     if (!paged_ok(p)) return false;
     if (p->n_q_heads < p->n_kv_heads || p->n_q_heads > 65535 || p->n_q_heads % p->n_kv_heads) return false;
-    if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return false;
+    if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale * kLog2e)) return false;
     A = AttendPlan{};
     A.G = p->n_q_heads / p->n_kv_heads;
     A.generic = p->impl == GRAPHKV_IMPL_GENERIC || !attend_mfma_applies(p->dtype, p->head_dim);
@@ -910,7 +913,7 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
     a.out = out;
     a.lse = lse;
     a.G = A.G;
-    a.c = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
+    a.c = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
     hipStream_t st = (hipStream_t)stream;
     if (A.generic) {
         GKV_LAUNCH(GRAPHKV_K_ATTEND_GENERIC, launch_attend_generic(a, p->dtype, p->page_format, st));

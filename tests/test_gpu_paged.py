@@ -167,6 +167,42 @@ def test_long_offsets():
     assert torch.equal(outs[0], outs[1])
 
 
+@pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
+def test_most_rows(impl):
+    """Sequences that lie at the end of the most rows that a call takes: theirs are written, read and attended to, no other is
+    touched."""
+    say("most rows")
+    rows, d = (1 << 24) - 1, 8
+    p = gk.PagedParams(n_kv_heads=1, n_q_heads=1, head_dim=d, page_tokens=4, n_pages=6, n_seqs=2, table_pages=3, n_rows=rows,
+                       max_rows=3, impl=impl)
+    table = torch.tensor([[4, 1, 0], [2, 5, 3]], dtype=torch.int32, device="cuda")
+    length = torch.tensor([2, 3], dtype=torch.int32, device="cuda")
+    start = torch.tensor([rows - 5, rows - 3, rows], dtype=torch.int32, device="cuda")
+    K, V, Q = (torch.zeros(rows, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    g = torch.Generator().manual_seed(11)
+    for t in (K, V, Q):
+        t[-5:] = torch.randn(5, 1, d, generator=g).to(torch.bfloat16).cuda()
+    pools = [torch.full((6, 1, 4, d), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    gk.graphkv_cache_write(p, K, V, *pools, table, length, start)
+    for pool, x in zip(pools, (K, V)):
+        want = torch.full((6, 1, 4, d), 9.0, dtype=torch.bfloat16)
+        want[4, 0, :2], want[2, 0, :3] = x[-5:-3, 0].cpu(), x[-3:, 0].cpu()
+        assert torch.equal(bits(pool), bits(want))
+    back = [torch.full((rows, 1, d), -7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    gk.graphkv_cache_read(p, *pools, table, length, start, K=back[0], V=back[1])
+    out = torch.full((rows, 1, d), -7.0, dtype=torch.bfloat16, device="cuda")
+    gk.graphkv_attend(p, Q, *pools, table, length, start, out=out)
+    for t in (*back, out):
+        assert bool((t[:-5] == -7).all())
+    assert torch.equal(bits(back[0][-5:]), bits(K[-5:])) and torch.equal(bits(back[1][-5:]), bits(V[-5:]))
+    for a, n in ((rows - 5, 2), (rows - 3, 3)):
+        k, v, q = (t[a:a + n, 0].cpu().double() for t in (K, V, Q))
+        x = (q @ k.T / math.sqrt(d)).masked_fill(torch.ones(n, n).triu(1).bool(), -math.inf)
+        want = torch.softmax(x, 1) @ v
+        # weights and output are rounded to bf16, half a step each (and 32-bit sums of at most 8 and 3 terms, far below)
+        assert bool(((out[a:a + n, 0].cpu().double() - want).abs() <= 2 ** -7 * 1.01 * v.abs().max()).all())
+
+
 # ---- attention --------------------------------------------------------------------------------------
 
 def run_attend(b, Q, **kw):

@@ -85,6 +85,22 @@ def test_strides_are_checked(lib, strides):
     assert calls(lib, good().c((0, 0), strides))["attend"] == -1
 
 
+@pytest.mark.parametrize("kw", [dict(n_rows=1 << 24), dict(n_rows=1 << 26)])
+def test_rows_beyond_a_launch_are_refused(lib, kw):
+    """A launch has at most 2^32 - 1 threads a dimension."""
+    assert set(calls(lib, good(**kw).c()).values()) == {-1}
+    assert gk.graphkv_attend_workspace_bytes(good(**kw)) == 0
+    assert gk.graphkv_attend_workspace_bytes(good(n_rows=(1 << 24) - 1)) > 0
+
+
+def test_sizes_that_overflow_are_refused(lib):
+    """A scale whose product with log2 e is no number of 32 bits; strides whose product with the rows is none of 64."""
+    assert calls(lib, good(softmax_scale=3e38).c())["attend"] == -1
+    assert gk.graphkv_attend_workspace_bytes(good(softmax_scale=2.0 ** 127)) > 0
+    for strides in (((1 << 38) + 8, 128), (128, (1 << 38) + 8)):
+        assert set(calls(lib, good().c(strides)).values()) == {-1}
+
+
 def test_outputs_must_not_overlap(lib):
     """Rows that lie within one another's heads are an output's mistake; inputs may be read that way."""
     d = 128
