@@ -16,7 +16,7 @@ namespace gkv {
 namespace {
 
 template <typename T, int FORM, int D, int NB, int RG>
-__global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void attend_many_kernel(AttendArgs a, ManyPlan pl)
+__global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void attend_many_kernel(AttendArgs a, ManyPlan pl)
 {
     constexpr int KS = 4 / RG, KEYS = 32 * NB * KS, DB = D / 32, R = 32 * RG;
     using L = Tile<T, FORM, D, KEYS, 256>;
@@ -280,10 +280,15 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
     p.join.slot_floats = p.block_rows * (D + 2);
     p.join.rows_per_wg = 8;
     const long blocks = (long)b.n_rows * G / p.block_rows + b.n_seqs;   // at least those of all sequences
-    // Units of 256 keys, or more where their number could pass 31 bits.
+    // Units of 256 keys with blocks of 64 rows, of 128 with larger ones, of 64 in fp32, whose tiles take longest; more where their
+    // number could pass 31 bits.  Shorter units share the work out better, longer ones leave fewer parts to be joined.  (us, units of
+    // 256 / 128 keys, eight key heads of four but for the last: 4 sequences of 12 rows over 2000 tokens 23 / 28, 500 rows over 8000 107 / 103, 500 over 500
+    // 32 / 29; fp32, 256 / 64 keys: 701 rows over 3000 and over 5000 tokens 962 / 888, 256 rows over 2000 117 / 122, d = 64 and eight
+    // heads, 300 over 900 34 / 30.)
     const long cap = (long)b.table_pages << b.page_shift;
     long units = 0;
-    for (p.step = 256 / p.tile_keys;; p.step *= 2) {
+    const int keys = p.block_rows == 64 ? 256 : dtype == 0 ? 64 : 128;
+    for (p.step = keys / p.tile_keys;; p.step *= 2) {
         units = (blocks / 2 + b.n_seqs) * (2 * (cap / ((long)p.tile_keys * p.step) + 1) + 2) * b.H;
         if (units <= INT32_MAX || p.tile_keys * p.step >= 1 << 29) break;
     }
