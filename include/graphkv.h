@@ -352,7 +352,8 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  *   lse  [n_rows, H_q]    out, optional (NULL), fp32
  *   ws   graphkv_attend_workspace_bytes(p) bytes, 256-byte aligned
  * Softmax statistics and sums are held in 32 bits; with bf16 rows the weights are
- * rounded to bf16 for the product with the values.  A row that sees nothing has
+ * rounded to bf16 for the product with the values.  (Sums of values beyond 2^100
+ * may leave the range of 32 bits.)  A row that sees nothing has
  * out = 0 and lse = -infinity.  What lies in places that a row does not see (later
  * positions, the rest of a page) has no influence on it, whatever its bits.
  * Results are deterministic; a sequence's may differ in their last bits with the

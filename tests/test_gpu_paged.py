@@ -391,6 +391,24 @@ def test_attention_with_large_logits_and_a_scale():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rise", [0.03, 0.07, 0.4, -0.07])
+def test_attention_with_rising_logits(dtype, rise):
+    """Logits that grow, or shrink, from key to key: by less than the running reference of the softmax may stay behind from tile to
+    tile, by about as much, by far more."""
+    say(f"rising logits dtype={dtype} rise={rise}")
+    for pairs, G, d in (([(1, 900), (3, 500)], 4, 128), ([(12, 700)], 4, 128), ([(30, 600)], 4, 64), ([(80, 500)], 4, 128)):
+        b = pu.Batch(pairs, H=2, G=G, d=d, ps=32, dtype=dtype, seed=5)
+        for s, (_, n) in enumerate(pairs):
+            for pos in range(n):
+                page, at = b.place(s, pos)
+                b.pool["K"][page, :, at, 0] = rise * pos
+        Q = b.random_rows(2 * G)
+        Q[:, :, 0] = math.sqrt(d)
+        out, lse = run_attend(b, Q)
+        pu.check_attend(b, Q, out, lse)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_attention_of_many_sequences(dtype):
     """More sequences than a workgroup has threads, most of them short, some without new rows."""
     say(f"many sequences dtype={dtype}")
