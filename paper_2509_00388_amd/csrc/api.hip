@@ -395,6 +395,11 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
         A.many_slots = A.many_records + align_up(join_record_bytes(A.mp.join));
         A.total = A.many_slots + align_up(join_slot_bytes(A.mp.join));
     }
+    // The parts that both leave are joined in one launch, whose width is that of the kernel with more pieces of a block: 16 each.  (us, a chunk
+    // of 500 rows beside 12 steps of 16 heads in fp8 / beside 63 of eight heads of four: two launches 112.5 / 214, one of 32 pieces a block 109 / 209, of
+    // 16 105 / 203, of 32 and 16 110 / 211.)
+    if (A.few && A.many)
+        for (JoinPlan *j : {&A.fp.join, &A.mp.join}) j->rows_per_wg = (j->slot_rows + 15) / 16;
     return true;
 }
 
@@ -923,15 +928,14 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
         A.fp.join.records = at<JoinRecord>(ws, 0);
         A.fp.join.slots = at<float>(ws, A.few_slots);
         GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, st));
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, p->dtype, st));
     }
     if (A.many) {
         A.mp.join.records = at<JoinRecord>(ws, A.many_records);
         A.mp.join.slots = at<float>(ws, A.many_slots);
         GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, st)
                                                     : launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.mp.join, p->dtype, st));
     }
+    GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, A.mp.join, p->dtype, st));
     return GRAPHKV_OK;
 }
 

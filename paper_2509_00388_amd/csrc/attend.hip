@@ -74,15 +74,17 @@ __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
 }
 
 // The parts of blocks of rows that several workgroups hold, put together: workgroup (y, w) takes rows y * rows_per_wg and on of the
-// block whose first part workgroup w held (in this order, so that the few w that hold one spread over all XCDs).  A row is 256 / GROUPS lanes wide, four sums a lane; where the parts are many, several
+// block whose first part workgroup w of the kernel for few rows, or behind those of the one for many, held (in this order, so that the few w that hold one spread over all XCDs).  A row is 256 / GROUPS lanes wide, four sums a lane; where the parts are many, several
 // groups of lanes share a row's.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan pl)
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan few, JoinPlan many)
 {
     constexpr int LANES = D / 4, GROUPS = 256 / LANES;
     __shared__ float4 sums[GROUPS][LANES];
     __shared__ float totals[GROUPS];
-    const int me = blockIdx.y;
+    const bool second = (int)blockIdx.y >= few.n_wg;
+    const JoinPlan pl = second ? many : few;
+    const int me = blockIdx.y - (second ? few.n_wg : 0);
     const JoinRecord rec = pl.records[me];
     const int first = blockIdx.x * pl.rows_per_wg, last = min(first + pl.rows_per_wg, rec.rows);
     if (rec.parts == 0 || first >= last) return;
@@ -142,11 +144,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, JoinPlan
 
 }  // namespace
 
-hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &pl, int dtype, hipStream_t st)
+hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &few, const JoinPlan &many, int dtype, hipStream_t st)
 {
-    const dim3 grid((pl.slot_rows + pl.rows_per_wg - 1) / pl.rows_per_wg, pl.n_wg);
+    auto chunks = [](const JoinPlan &p) { return p.n_wg ? (p.slot_rows + p.rows_per_wg - 1) / p.rows_per_wg : 0; };
+    const dim3 grid(max(chunks(few), chunks(many)), few.n_wg + many.n_wg);
     const int D = attend_width(a.b.d);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, pl); return hipGetLastError(); };
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, few, many); return hipGetLastError(); };
     if (dtype == 0) return D == 64 ? go(attend_join_kernel<float, 64>) : go(attend_join_kernel<float, 128>);
     return D == 64 ? go(attend_join_kernel<uint16_t, 64>) : D == 128 ? go(attend_join_kernel<uint16_t, 128>) : go(attend_join_kernel<uint16_t, 256>);
 }

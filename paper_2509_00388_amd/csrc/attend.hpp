@@ -190,7 +190,7 @@ hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipSt
 hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_wide(const AttendArgs &a, const ManyPlan &pl, int form, hipStream_t st);
-hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &pl, int dtype, hipStream_t st);
+hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &few, const JoinPlan &many, int dtype, hipStream_t st);   // n_wg 0: none
 inline size_t join_record_bytes(const JoinPlan &p) { return (size_t)p.n_wg * sizeof(JoinRecord); }
 inline size_t join_slot_bytes(const JoinPlan &p) { return (size_t)2 * p.n_wg * p.slot_floats * 4; }
 
