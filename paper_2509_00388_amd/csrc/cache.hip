@@ -1,6 +1,7 @@
 // Rows written to the pages of a cache and read back (graphkv_cache_write, graphkv_cache_read).
 //
-// A wave takes a row with all its heads, so that the row's sequence and page are looked up once; a head's values lie in as
+// A wave takes a row with all its heads, so that the row's sequence and page are looked up once, or, where rows are few, some of its heads
+// (turns_grid()); a head's values lie in as
 // many lanes as it has 16-byte pieces (a power of two, at most 64, a second turn for the rest).  Both kernels are bound by
 // memory: every byte is moved once, with 16-byte accesses on the wider side.  Measured (bf16 rows, eight heads of 128, pages of 64,
 // fp8): 32768 rows written in 44 us and read back in 46, 204 MB, at 4.6 and 4.4 TB/s, where a copy of 4 GiB reaches 4.6;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(PagedBatch b, const T 
     if (row < q.row0 || row >= q.row0 + q.n || pos < 0) return;
     const int page = page_of(b, s, pos);
     if (page < 0) return;
-    for (int h = lane / group; h < b.H; h += heads) {
+    for (int h = lane / group + heads * blockIdx.y; h < b.H; h += heads * gridDim.y) {
         const T *k = K + row * row_stride + h * head_stride, *v = V + row * row_stride + h * head_stride;
         uint4 kv[TURNS], vv[TURNS];
 #pragma unroll
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(PagedBatch b, const voi
     const int pos = q.len - q.n + (row - q.row0);
     if (row < q.row0 || row >= q.row0 + q.n) return;
     const int page = pos < 0 ? -1 : page_of(b, s, pos);
-    for (int h = lane / group; h < b.H; h += heads) {
+    for (int h = lane / group + heads * blockIdx.y; h < b.H; h += heads * gridDim.y) {
         const long from = pool_row(b, max(page, 0), h, max(pos, 0));
         for (int p = at; p < pieces; p += group) {
             uint4 kv = reinterpret_cast<const uint4 *>(Kpages)[from * pieces + p];
@@ -186,6 +187,15 @@ int lanes_for(int pieces)
     return g;
 }
 
+// Four rows a workgroup; the turns that a wave would take over a row's heads, one load after the other, are dealt to several waves
+// as long as the card has room for them at once, 8192 in 256 compute units.  (us, one wave a row / dealt: 2011 fp32 rows of 16 heads of 64
+// written as int8 11.6 / 9.5; a call for 256 bf16 rows of 32 heads of 128 20.7 / 13.2.)
+dim3 turns_grid(const PagedBatch &b, int group)
+{
+    const int turns = (b.H * group + kWave - 1) / kWave, room = 8192 / b.n_rows;
+    return dim3((b.n_rows + 3) / 4, room < 1 ? 1 : room < turns ? room : turns);
+}
+
 }  // namespace
 
 template <typename T, int FORM>
@@ -193,7 +203,7 @@ static hipError_t write_rows(const PagedBatch &b, const void *K, const void *V, 
                              void *Kpages, void *Vpages, float *Kscale, float *Vscale, hipStream_t st)
 {
     const int pieces = b.d / Elem<T>::kPerVec, group = lanes_for(pieces);
-    const dim3 grid((b.n_rows + 3) / 4);
+    const dim3 grid = turns_grid(b, group);
     if (pieces <= kWave)
         cache_write_kernel<T, FORM, 1><<<grid, 256, 0, st>>>(b, (const T *)K, (const T *)V, row_stride, head_stride, Kpages,
                                                              Vpages, Kscale, Vscale, group);
@@ -219,7 +229,7 @@ static hipError_t read_rows(const PagedBatch &b, const void *Kpages, const void 
                             const float *Vscale, void *K, void *V, long row_stride, long head_stride, hipStream_t st)
 {
     const int group = lanes_for(b.d / Cached<T, FORM>::kPerVec);
-    cache_read_kernel<T, FORM><<<dim3((b.n_rows + 3) / 4), 256, 0, st>>>(b, Kpages, Vpages, Kscale, Vscale, (T *)K, (T *)V,
+    cache_read_kernel<T, FORM><<<turns_grid(b, group), 256, 0, st>>>(b, Kpages, Vpages, Kscale, Vscale, (T *)K, (T *)V,
                                                                         row_stride, head_stride, group);
     return hipGetLastError();
 }
