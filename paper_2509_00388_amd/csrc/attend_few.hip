@@ -6,6 +6,11 @@
 // 16-byte loads of the next tile in flight while this one is multiplied, and keeps its own running maximum, sum and O^T:
 // no barrier until the stretch of a pair ends and the waves' parts are joined.  A pair that one workgroup holds whole is
 // finished there; the parts of others go to scratch memory and are joined by a second launch.
+//
+// Measured (bf16 rows, d = 128, eight key heads of four): one token over 131072 keys 97 us, 5.5 TB/s (reading alone is faster than the 4.6 of
+// a copy); 64 tokens over 400 to 5000 keys each in fp8 pages 93 us, 4.2 TB/s, where decode and the LDS share the time; one token
+// over 2048 keys 8.6 us, a chain of look-ups, loads, two products and the join of the waves with a tile a workgroup.  Slower: three workgroups
+// a compute unit, 768 or 1024 of them in all, 64 keys a wave.
 #include "attend_tile.hpp"
 #include "kernels.hpp"
 

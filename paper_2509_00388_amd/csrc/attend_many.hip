@@ -8,6 +8,10 @@
 // the tile's keys each, and their sums are joined at the end.  Logits stay in registers: each wave turns its 32 x 32 NB of
 // them into weights and multiplies them with the values (attend_tile.hpp).  The work is cut into equal stretches, whatever
 // the lengths (attend.hpp); parts of blocks that several workgroups hold are joined by a second launch.
+//
+// Measured: 16 sequences of eight tokens, seven query heads of each of four key heads, 1000 to 9000 keys of 128 in int8: 42 us, 2.9 TB/s, bound by the issue of
+// vector instructions (27 a matrix instruction, a third of them decode); with two tiles on their way instead of one the same.  701 fp32 rows of 16 heads of 64
+// over 2000 and over 5000 keys 206 us, 97 TFLOP/s of the 153 that a library product of 8192 cubed reaches.
 #include "attend_tile.hpp"
 #include "kernels.hpp"
 
