@@ -25,7 +25,7 @@ template <typename T, int FORM, int D, int NB> struct WavePlace {
 };
 
 template <typename T, int FORM, int D, int NB>
-__global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void attend_few_kernel(AttendArgs a, FewPlan pl)
+__global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void attend_few_kernel(AttendArgs a, FewPlan pl)
 {
     constexpr int KEYS = 32 * NB, DB = D / 32;
     using L = Tile<T, FORM, D, KEYS, 64>;
@@ -249,8 +249,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || D > 128) ? 1 : 2) void atte
     }
 }
 
-// 32-key blocks of a wave's share of a tile: as many as put 8 KiB of keys in flight.
-template <typename T, int FORM, int D> constexpr int blocks_of() { return D <= 64 ? 2 : 1; }
+// 32-key blocks of a wave's share of a tile: as many as put 8 KiB of keys in flight.  (fp32 rows of 64, us, two blocks, which leave one workgroup a compute
+// unit for their registers, / one: a token over 65536 keys 89 / 73, 64 tokens over 1000 to 5000 231 / 176.)
+constexpr int few_blocks(int D, bool wide_rows) { return D <= 64 && !wide_rows ? 2 : 1; }   // wide_rows: cached in 32 bits
+template <typename T, int FORM, int D> constexpr int blocks_of() { return few_blocks(D, FORM == kPagesPlain && sizeof(T) == 4); }
 
 template <typename T, int FORM, int D>
 hipError_t go_few(const AttendArgs &a, const FewPlan &pl, hipStream_t st)
@@ -282,7 +284,7 @@ FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G)
 {
     const int D = attend_width(b.d);
     FewPlan p{};
-    p.tile_keys = 4 * 32 * (D <= 64 ? 2 : 1);
+    p.tile_keys = 4 * 32 * few_blocks(D, form == kPagesPlain && dtype == 0);
     const long rows = (long)b.max_rows * G;
     p.join.slot_rows = rows < kFewRows ? (int)rows : kFewRows;
     p.join.slot_floats = (p.join.slot_rows * (D + 2) + 3) & ~3;
