@@ -524,6 +524,34 @@ def test_captured_calls_follow_the_lengths(pairs, d, form):
             assert torch.equal(bits(x), bits(y))
 
 
+def test_graphs_that_share_a_workspace():
+    """Captured calls of either kernel, of both and of blocks of each size leave nothing in the workspace that the next one would
+    take for its own: replayed in turn, with eager calls on the same workspace between."""
+    say("graphs that share a workspace")
+    sets = []
+    for seed, pairs in ((1, [(1, 3000), (1, 5), (1, 900)]), (2, [(60, 500), (1, 700)]), (3, [(1, 300)] * 9 + [(70, 400), (4, 90)]), (4, [(14, 800)])):
+        b = pu.Batch(pairs, H=2, G=4, d=128, ps=16, seed=seed)
+        sets.append((b, on_gpu(b.random_rows(8)), b.device()))
+    ws = torch.randint(0, 256, (max(gk.graphkv_attend_workspace_bytes(b.p) for b, _, _ in sets),), dtype=torch.uint8, device="cuda")
+    want = [gk.graphkv_attend(b.p, Q, *args) for b, Q, args in sets]
+    torch.cuda.synchronize()
+    graphs = []
+    for b, Q, args in sets:
+        out, graph = torch.zeros_like(Q), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            gk.graphkv_attend(b.p, Q, *args, out=out, ws=ws)
+        graphs.append((graph, out))
+    for turn in ([0, 1, 2, 3], [3, 2, 1, 0], [2, 2, 0, 3, 1]):
+        for i in turn:
+            graphs[i][1].zero_()
+            graphs[i][0].replay()
+            b, Q, args = sets[(i + 1) % len(sets)]
+            assert torch.equal(gk.graphkv_attend(b.p, Q, *args, ws=ws), want[(i + 1) % len(sets)])
+        torch.cuda.synchronize()
+        for i in turn:
+            assert torch.equal(graphs[i][1], want[i]), (turn, i)
+
+
 def test_two_streams_with_a_workspace_each():
     say("two streams")
     sets = []
