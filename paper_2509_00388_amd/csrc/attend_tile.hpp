@@ -248,14 +248,17 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
     top = fmaxf(m, other_half_max(top) * c);   // (c > 0)
+    // (The vote only says whether any row has something to do: each row's reference follows its own maxima, so that how its weights are rounded
+    // does not depend on what other rows see.)
     if (__any(top > m + kMaxLag)) {
-        const float fade = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        const bool grown = top > m + kMaxLag;
+        const float fade = grown ? __builtin_amdgcn_exp2f(m - top) : 1.f;
         l *= fade;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] *= fade;
-        m = top;
+        m = grown ? top : m;
     }
     const float shift = m == -INFINITY ? 0.f : m;   // (nothing seen yet: all weights are 2^-inf)
 #pragma unroll

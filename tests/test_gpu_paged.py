@@ -408,6 +408,52 @@ def test_attention_with_rising_logits(dtype, rise):
         pu.check_attend(b, Q, out, lse)
 
 
+# (stacked rows: 32, 8, 48, 120, 320; which kernel takes them goes by the type of the rows and d too)
+OTHERS = [([(8, 500)], 4, 128), ([(4, 300)], 2, 64), ([(12, 700)], 4, 128), ([(30, 600)], 4, 64), ([(30, 600)], 4, 128), ([(80, 500)], 4, 128),
+          ([(80, 500)], 4, 64), ([(40, 300)], 1, 256)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("shape", range(len(OTHERS)))
+def test_attention_does_not_depend_on_other_rows(dtype, form, shape):
+    """Logits that grow a little from key to key, so that the running reference of a softmax may stay behind: a large finite key at a late
+    position, or other queries of the later rows, leave the earlier rows' bits as they are."""
+    pairs, G, d = OTHERS[shape]
+    say(f"other rows dtype={dtype} form={form} {pairs} G={G} d={d}")
+    (n, length), = pairs
+    for rise in (0.004, 0.012, 0.03):
+        b = pu.Batch(pairs + [(1, 32)], H=2, G=G, d=d, ps=32, dtype=dtype, form=form, seed=shape, table_pages=4096)
+        b.len[1] = 4096 * 32   # (beside a long sequence a workgroup's stretch holds several tiles of the first one)
+        keys = torch.randn(b.p.n_pages, 2, 32, d, generator=b.g)
+        for pos in range(length):
+            page, at = b.place(0, pos)
+            keys[page, :, at, 0] = rise * pos
+        b.set_pool("K", keys.to(b.p.torch_dtype))
+        Q = b.random_rows(2 * G)
+        Q[:, :, 0] = math.sqrt(d)
+        clean, clean_lse = run_attend(b, Q)
+        if rise == 0.03:
+            pu.check_attend(b, Q, clean, clean_lse)
+        for late in (length - n + n // 2, length - 2):
+            before = late - (length - n)   # rows of the sequence that do not see the late position
+            page, at = b.place(0, late)
+            own_key = keys[page, :, at].clone()
+            for value in (60.0, 3000.0, math.inf) if form == gk.PAGES_PLAIN else (60.0, 3000.0):
+                keys[page, :, at] = 0
+                keys[page, :, at, 0] = value
+                b.set_pool("K", keys.to(b.p.torch_dtype))
+                out, lse = run_attend(b, Q)
+                assert torch.equal(out[:before], clean[:before]) and torch.equal(lse[:before], clean_lse[:before]), (rise, late, value)
+                assert not torch.equal(lse[before:n], clean_lse[before:n])
+            keys[page, :, at] = own_key
+            b.set_pool("K", keys.to(b.p.torch_dtype))
+            other = Q.clone()
+            other[before:n] *= 7
+            out, lse = run_attend(b, other)
+            assert torch.equal(out[:before], clean[:before]) and torch.equal(lse[:before], clean_lse[:before]), (rise, late)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_of_many_sequences(dtype):
     """More sequences than a workgroup has threads, most of them short, some without new rows."""
