@@ -118,6 +118,31 @@ def test_codes_next_to_borders(dtype, form):
     check_write(b, K, V)
 
 
+def test_integer_codes_are_rounded_once():
+    """Products of integer codes and scales of all 24 bits that lie next to the middle of two bf16 numbers: to 32 bits they round onto it."""
+    say("integer codes rounded once")
+    H, d, ps, n = 4, 64, 32, 512
+    b = pu.Batch([(n, n)], H=H, d=d, ps=ps, form=gk.PAGES_INT8, seed=21)
+    code = torch.randint(3, 128, (b.p.n_pages, H, ps), generator=b.g)
+    middle = (257 + 2 * torch.randint(0, 128, code.shape, generator=b.g)).double() / 512 * 2.0 ** torch.randint(-20, 20, code.shape, generator=b.g)
+    for name in "KV":
+        b.pool[name] = torch.randint(-127, 128, (b.p.n_pages, H, ps, d), generator=b.g).to(torch.int8)
+        b.pool[name][..., 0::4] = code[..., None].to(torch.int8)
+        b.pool[name][..., 2::8] = -code[..., None].to(torch.int8)
+        b.pool[name + "s"] = (middle / code).float()
+    K, V = gk.graphkv_cache_read(b.p, *b.device())
+    twice = 0
+    for got, name in ((K, "K"), (V, "V")):
+        for r, s, pos in b.each_row():
+            page, at = b.place(s, pos)
+            x = b.pool[name][page, :, at].double() * b.pool[name + "s"][page, :, at].double()[:, None]   # exact
+            m, e = torch.frexp(x)
+            want = torch.ldexp(torch.round(m * 256) / 256, e)   # 8 bits, ties to even
+            assert torch.equal(got[r].cpu().double(), want), (name, r)
+            twice += int((x.float().to(torch.bfloat16).double() != want).sum())
+    assert twice > 1000
+
+
 def test_rows_without_a_place():
     """Page numbers outside the pool, rows that come before a sequence's first token, lengths beyond the table: not written,
     read as zeros; nothing else changes."""
