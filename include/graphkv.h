@@ -301,8 +301,8 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
 enum { GRAPHKV_PAGES_PLAIN = 0, GRAPHKV_PAGES_FP8 = 1, GRAPHKV_PAGES_INT8 = 2 };
 
 typedef struct graphkv_paged_params {
-    int32_t n_kv_heads;    /* H_kv >= 1                                                  */
-    int32_t n_q_heads;     /* H_q, a multiple of H_kv (attend only)                      */
+    int32_t n_kv_heads;    /* H_kv, 1 .. 65535                                           */
+    int32_t n_q_heads;     /* H_q, a multiple of H_kv, <= 65535 (attend only)            */
     int32_t head_dim;      /* d, a multiple of 8 (16 with 8-bit pages), <= 512           */
     int32_t dtype;         /* GRAPHKV_FP32 / GRAPHKV_BF16: type of the rows K, V, Q, out */
     int32_t page_format;   /* GRAPHKV_PAGES_*                                            */
@@ -351,6 +351,12 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  *        overlap
  *   lse  [n_rows, H_q]    out, optional (NULL), fp32
  *   ws   graphkv_attend_workspace_bytes(p) bytes, 256-byte aligned
+ * Work is counted in 32 bits: where the matrix-core kernels run (AUTO, d up to 256 for bf16
+ * and 128 for fp32), params are refused with n_rows * H_q / H_kv > 2^30, with n_rows * H_q + 192 *
+ * n_seqs * H_kv >= 2^35, or, if some sequences may go to the kernel for few rows (max_rows * H_q / H_kv
+ * <= 32, or 8 sequences and more), with n_seqs * H_kv * ceil(table_pages * page_tokens / 128) >= 2^31.
+ * graphkv_attend_workspace_bytes() is 0 for params that are refused, and where no scratch
+ * memory is needed: by the scalar kernel, and without rows or sequences.
  * Softmax statistics and sums are held in 32 bits; with bf16 rows the weights are
  * rounded to bf16 for the product with the values.  (Sums of values beyond 2^100
  * may leave the range of 32 bits.)  A row that sees nothing has

@@ -372,10 +372,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     A.generic = p->impl == GRAPHKV_IMPL_GENERIC || !attend_mfma_applies(p->dtype, p->head_dim);
     const PagedBatch b = batch_of(p, nullptr, nullptr, nullptr);
     if (A.generic || b.n_rows == 0 || b.n_seqs == 0) return true;
-    // (key tiles of all sequences and heads, and the workgroups of the largest launch, are counted in 32 bits)
-    const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
-    if (((tokens + 127) / 128) * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
-    if ((int64_t)p->n_rows * A.G > (1 << 30)) return false;   // (and so are stacked rows)
+    if ((int64_t)p->n_rows * A.G > (1 << 30)) return false;   // (stacked rows are counted in 32 bits)
     // Sequences of few rows and of many go to different kernels where there are enough of both for two more launches: from eight
     // sequences on, unless the rows are as many as if all of them were as long as they may be (which the device alone knows: either
     // kernel for many rows takes any).  (A chunk of 500 rows beside steps over 2000 to 5000 tokens, eight key heads of four, us for one kernel
@@ -384,6 +381,9 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     A.many = (int64_t)b.max_rows * A.G > kFewRows;
     A.few = !A.many || (b.n_seqs >= 8 && (int64_t)b.n_seqs * b.max_rows > b.n_rows);
     if (A.few) {
+        // (and so are the key tiles of all sequences and heads, at least 128 keys each)
+        const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
+        if ((tokens + 127) / 128 * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
         A.fp = few_plan(b, p->dtype, p->page_format, A.G);
         A.few_slots = align_up(join_record_bytes(A.fp.join));
         A.total = A.few_slots + align_up(join_slot_bytes(A.fp.join));

@@ -492,6 +492,17 @@ def test_attention_of_many_sequences(dtype):
     pu.check_attend(b, Q, out, lse)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_over_the_longest_tables(dtype):
+    """Tables of 2^30 tokens with more heads and sequences than the kernel for few rows would count, which takes none of them."""
+    say(f"longest tables dtype={dtype}")
+    b = pu.Batch([(40, 100), (40, 1500), (33, 33), (1, 0)], H=64, G=1, d=16, ps=1024, dtype=dtype, table_pages=1 << 20, behind=1)
+    assert b.p.table_pages * b.ps == 1 << 30 and 4 * 64 * (1 << 30) // 128 >= 1 << 31
+    Q = b.random_rows(64)
+    out, lse = run_attend(b, Q)
+    pu.check_attend(b, Q, out, lse)
+
+
 # ---- together, in graphs, on streams ----------------------------------------------------------------
 
 def test_prefill_evict_decode():

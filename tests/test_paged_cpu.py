@@ -187,3 +187,29 @@ def test_definition_of_attention():
             assert torch.allclose(out[rows, h], torch.softmax(x, 1) @ v, rtol=1e-12, atol=1e-12)
             assert torch.allclose(lse[rows, h], torch.logsumexp(x, 1), rtol=1e-12, atol=1e-12)
     assert float(bound[1:-1].max()) < 1e-3
+
+
+@pytest.mark.parametrize("kw", [dict(n_kv_heads=64, n_q_heads=256, n_pages=1000, page_tokens=1024, table_pages=1 << 20),
+                                dict(n_kv_heads=128, n_q_heads=128, n_seqs=7, n_rows=400, max_rows=100, page_tokens=1, table_pages=1 << 30),
+                                dict(n_kv_heads=1, n_q_heads=64, n_rows=1 << 24, max_rows=0, n_seqs=1),
+                                dict(n_kv_heads=8, n_q_heads=8, n_rows=1 << 20, max_rows=1, n_seqs=1 << 20, table_pages=255)])
+def test_sizes_up_to_the_stated_limits_are_taken(lib, kw):
+    """Long tables beside rows that only the kernels for many rows take, the most stacked rows, the most sequences."""
+    if kw.get("n_rows") == 1 << 24:
+        kw = dict(kw, n_rows=(1 << 24) - 1)
+    p = good(**kw)
+    G = p.n_q_heads // p.n_kv_heads
+    most = p.max_rows or p.n_rows
+    assert p.n_rows * G <= 1 << 30 and p.n_rows * p.n_q_heads + 192 * p.n_seqs * p.n_kv_heads < 1 << 35
+    if most * G <= 32 or p.n_seqs >= 8:
+        assert p.n_seqs * p.n_kv_heads * -(-p.table_pages * p.page_tokens // 128) < 1 << 31
+    need = gk.graphkv_attend_workspace_bytes(p)
+    assert 0 < need < 256 << 20
+    assert lib.graphkv_attend(ctypes.byref(p.c()), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, need - 1, None) == -2
+
+
+@pytest.mark.parametrize("kw", [dict(n_kv_heads=1, n_q_heads=128, n_rows=(1 << 23) + 1),
+                                dict(n_kv_heads=8, n_q_heads=8, n_rows=1 << 20, max_rows=1, n_seqs=1 << 20, table_pages=513, page_tokens=64)])
+def test_sizes_beyond_the_stated_limits_are_refused(lib, kw):
+    p = good(**kw)
+    assert gk.graphkv_attend_workspace_bytes(p) == 0 and calls(lib, p.c())["attend"] == -1
