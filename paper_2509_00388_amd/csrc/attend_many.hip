@@ -199,7 +199,8 @@ __global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void attend_many_
         if (tid == 0 && u0 == 0 && u1 < units)
             pl.join.records[me] = {stretch_owner(total, pos + units - 1, n_wg) - me + 1, 2 * me + (pos == mine ? 0 : 1), sq.row0, h, row0,
                                    min(R, rows - row0)};
-        const int r = 32 * group + l32;
+        int r = 32 * group + l32;
+        asm volatile("" : "+v"(r));   // (nor are the places of its results: fp8 rows of 128 in blocks of 128 rows spilled)
         if (stream == 0 && row0 + r < rows) {
             if (u0 > 0 || u1 < units) {
                 float *slot = pl.join.slots + (size_t)(2 * me + (pos == mine ? 0 : 1)) * pl.join.slot_floats;

@@ -54,3 +54,15 @@ def test_kernels_hide_their_loads_behind_other_waves(kernels, kernel, waves, var
     for name, k in some.items():
         assert int(k["vgpr_count"]) <= 512 // waves // 8 * 8, (name, k["vgpr_count"])
         assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
+
+
+@pytest.mark.parametrize("kernel,waves,variants", [("attend_few_kernel", 1, 15), ("attend_many_kernel", 1, 24), ("attend_wide_kernel", 2, 6),
+                                                   ("attend_join_kernel", 4, 5), ("attend_generic_kernel", 4, 6),
+                                                   ("cache_write_kernel", 4, 12), ("cache_read_kernel", 4, 6)])
+def test_kernels_of_the_paged_cache_spill_nothing(kernels, kernel, waves, variants):
+    """Every variant keeps its values in registers, and leaves so many waves room on a SIMD (vector and accumulation registers together)."""
+    some = {name: k for name, k in kernels.items() if kernel in name}
+    assert len(some) == variants
+    for name, k in some.items():
+        assert int(k["vgpr_count"]) <= 512 // waves // 8 * 8, (name, k["vgpr_count"])
+        assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
