@@ -158,7 +158,11 @@ __global__ __launch_bounds__(256, D * sizeof(T) > 256 ? 1 : 2) void attend_few_k
             if constexpr (FORM != kPagesPlain) scale_weights<NB>(vs, all, seen, hh, p);
             wave_sync();
 #pragma unroll
-            for (int n = 0; n < NB; ++n) add_values<D, P::kPitch>(kv + 32 * n * P::kPitch, p[n], lane, o, T{});
+            for (int n = 0; n < NB; ++n) {
+                const unsigned char *vt = kv + 32 * n * P::kPitch;
+                if constexpr (sizeof(T) == 2 && FORM == kPagesPlain) add_values_twice<D, P::kPitch>(vt, p[n], lane, o);
+                else add_values<D, P::kPitch>(vt, p[n], lane, o, T{});
+            }
             wave_sync();
             vis = vis1;
             at = at1;

@@ -433,6 +433,24 @@ def test_attention_with_rising_logits(dtype, rise):
         pu.check_attend(b, Q, out, lse)
 
 
+@pytest.mark.parametrize("d", [64, 80, 128, 256])
+def test_attention_of_few_rows_keeps_the_weights(d):
+    """At most 32 stacked rows over plain pages in bf16: the weights go into the product with the values as two bf16 numbers each, so they
+    are off by half a step of the second, 2^-16 of the weight, not by 2^-8."""
+    say(f"weights of few rows d={d}")
+    b = pu.Batch([(1, 2), (1, 3), (1, 40), (2, 300), (8, 100), (3, 2), (1, 2000)], H=2, G=4, d=d, ps=16, before=1, behind=1, seed=d)
+    Q = b.random_rows(8)
+    out, lse = run_attend(b, Q)
+    pu.check_attend(b, Q, out, lse)
+    want, _, bound, _ = b.attend(Q)
+    values, b.pool["V"] = b.pool["V"], b.pool["V"].abs()
+    mass = b.attend(Q)[0]   # sums of the magnitudes
+    b.pool["V"] = values
+    mine = ~want.isnan()
+    allow = bound - (2.0 ** -8 - 2.0 ** -16) * mass
+    assert ((out.cpu().double() - want).abs() <= allow + 2.0 ** -100)[mine].all()
+
+
 # (stacked rows: 32, 8, 48, 120, 320; which kernel takes them goes by the type of the rows and d too)
 OTHERS = [([(8, 500)], 4, 128), ([(4, 300)], 2, 64), ([(12, 700)], 4, 128), ([(30, 600)], 4, 64), ([(30, 600)], 4, 128), ([(80, 500)], 4, 128),
           ([(80, 500)], 4, 64), ([(40, 300)], 1, 256)]
