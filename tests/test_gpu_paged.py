@@ -169,6 +169,82 @@ def test_rows_without_a_place():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pairs,G", [([(6, 30), (5, 90), (4, 50), (3, 20)], 2), ([(150, 200), (60, 100), (3, 40), (20, 20)], 2), ([(20, 90), (9, 9), (16, 70), (30, 40)], 4)])
+def test_row_numbers_outside_the_tensors(dtype, form, pairs, G):
+    """Row numbers that do not ascend or lie outside the tensors, as the header says what becomes of them: cut to the tensors and to
+    the most rows of a sequence.  Rows and places of no sequence keep what they hold; what exactly one sequence owns is right."""
+    say(f"row numbers dtype={dtype} form={form} {pairs}")
+    d, H = 32, 2
+    b = pu.Batch(pairs, H=H, G=G, d=d, ps=8, dtype=dtype, form=form, before=1, behind=2, seed=31)
+    rows, most = b.rows, b.p.max_rows
+    K, V, Q = b.random_rows(H), b.random_rows(H), b.random_rows(H * G)
+    k, v, c, u = b.values("K"), b.values("V"), 1 / math.sqrt(d), 2.0 ** -24
+    for start in ([-5, 3, 3, 900, 2], [7, 2, 1, 0, -1], [rows] * 5, [0, rows, 5, rows, 2 ** 31 - 1], [-2 ** 31, rows // 2, rows // 3, rows, 0],
+                  [rows - 1, 4, rows + 7, 9, rows - 2]):
+        b.start = torch.tensor(start, dtype=torch.int32)
+        spans = []
+        for s in range(4):
+            r0 = min(max(start[s], 0), rows)
+            spans.append((r0, min(min(max(start[s + 1], r0), rows) - r0, most)))
+        # write and read go by the row: its sequence is the number of those that end at or before it
+        owner = [sum(start[s + 1] <= r for s in range(4)) for r in range(rows)]
+        cells = {}
+        for r in range(rows):
+            s = owner[r]
+            if s < 4 and spans[s][0] <= r < sum(spans[s]):
+                cells[r] = b.place(s, int(b.len[s]) - spans[s][1] + r - spans[s][0])
+        args = b.device()
+        gk.graphkv_cache_write(b.p, on_gpu(K), on_gpu(V), *args)
+        for i, (name, x) in enumerate((("K", K), ("V", V))):
+            want = b.pool[name].clone()
+            code, scale = (x, None) if form == gk.PAGES_PLAIN else pu.encode(x, form)
+            code = code.to(torch.int8) if form == gk.PAGES_INT8 else code.float().to(torch.float8_e4m3fn) if form == gk.PAGES_FP8 else code
+            want_scale = None if scale is None else b.pool[name + "s"].clone()
+            for r, cell in cells.items():
+                if cell:
+                    want.view(torch.uint8)[cell[0], :, cell[1]] = code[r].contiguous().view(torch.uint8)
+                    if scale is not None:
+                        want_scale[cell[0], :, cell[1]] = scale[r].float()
+            assert torch.equal(bits(args[i]), bits(want)), (start, name)
+            assert scale is None or torch.equal(bits(args[5 + i]), bits(want_scale)), (start, name)
+        args = b.device()
+        back = [torch.full((rows, H, d), -7.0, dtype=b.p.torch_dtype, device="cuda") for _ in range(2)]
+        gk.graphkv_cache_read(b.p, *args, K=back[0], V=back[1])
+        for got, values in zip(back, (k, v)):
+            want = torch.full((rows, H, d), -7.0).to(b.p.torch_dtype)
+            for r, cell in cells.items():
+                want[r] = values[cell[0], :, cell[1]].to(b.p.torch_dtype) if cell else 0
+            assert torch.equal(got.cpu(), want), start
+        out = torch.full((rows, H * G, d), -7.0, dtype=b.p.torch_dtype, device="cuda")
+        lse = torch.full((rows, H * G), -7.0, device="cuda")
+        ws = torch.randint(0, 256, (gk.graphkv_attend_workspace_bytes(b.p),), dtype=torch.uint8, device="cuda")
+        gk.graphkv_attend(b.p, on_gpu(Q), *args, out=out, lse=lse, ws=ws)
+        out, lse = out.cpu().double(), lse.cpu()
+        for r in range(rows):
+            mine = [s for s in range(4) if spans[s][0] <= r < sum(spans[s])]
+            if not mine:
+                assert (out[r] == -7).all() and (lse[r] == -7).all(), (start, r)
+            if len(mine) != 1:
+                continue
+            s, = mine
+            pos = int(b.len[s]) - spans[s][1] + r - spans[s][0]
+            seen = [b.place(s, j) for j in range(pos + 1)]
+            if not seen:
+                assert (out[r] == 0).all() and (lse[r] == -math.inf).all(), (start, r)
+                continue
+            page, at = torch.tensor(seen).T
+            for h in range(H * G):
+                kk, vv = k[page, h // G, at], v[page, h // G, at]
+                q = Q[r, h].double()
+                w = torch.softmax(kk @ q * c, 0)
+                off = (d + 8) * u * float((kk.abs() @ q.abs()).max()) * c
+                half = pu.half_step(torch.bfloat16) if dtype == gk.BF16 else 0.0
+                allow = (w @ vv.abs()) * (half + 4 * off + 4 * (len(seen) + d + 64) * u) + (w @ vv).abs() * pu.half_step(b.p.torch_dtype)
+                assert ((out[r, h] - w @ vv).abs() <= allow).all(), (start, r, h)
+
+
 def test_long_offsets():
     """Places beyond 2^32 bytes of a pool."""
     say("long offsets")
