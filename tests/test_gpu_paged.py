@@ -586,6 +586,42 @@ def test_attention_of_many_sequences(dtype):
     pu.check_attend(b, Q, out, lse)
 
 
+LONG = [([(1, 9001)], 1, 4, 128), ([(8, 20000), (1, 30)], 1, 4, 128), ([(1, 70000), (1, 9)], 2, 1, 64), ([(1, 12000)], 1, 2, 256), ([(12, 9000)], 1, 4, 128),
+        ([(30, 10001)], 1, 4, 128), ([(100, 6000)], 1, 1, 64), ([(60, 12000), (5, 3000)], 1, 4, 128), ([(300, 4100)], 2, 1, 64), ([(40, 5000)], 1, 4, 256),
+        ([(1, 4000)] * 8 + [(200, 7000)], 1, 2, 128)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("shape", range(len(LONG)))
+def test_attention_over_many_parts(dtype, form, shape):
+    """Long sequences of few heads, whose keys are shared out among many workgroups and joined from as many parts, against the definition."""
+    pairs, H, G, d = LONG[shape]
+    say(f"many parts dtype={dtype} form={form} {LONG[shape]}")
+    b = pu.Batch(pairs, H=H, G=G, d=d, ps=64, dtype=dtype, form=form, seed=shape, before=1, behind=1)
+    Q = b.random_rows(H * G)
+    out, lse = run_attend(b, Q)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    k, v, c, u = b.values("K"), b.values("V"), 1 / math.sqrt(d), 2.0 ** -24
+    for s, (n, length) in enumerate(pairs):
+        pages = b.table[s, :-(-length // 64)].long()
+        r0 = int(b.start[s])
+        hidden = torch.arange(length)[None] > torch.arange(length - n, length)[:, None]
+        for h in range(H * G):
+            kk, vv = (x[pages, h // G].reshape(-1, d)[:length] for x in (k, v))
+            q = Q[r0:r0 + n, h].double()
+            x = (q @ kk.T * c).masked_fill(hidden, -math.inf)
+            w = torch.softmax(x, 1)
+            want, want_lse = w @ vv, torch.logsumexp(x, 1)
+            # as the tests of short sequences: logits, sums, weights and results, each with its rounding
+            off = (d + 8) * u * (q.abs() @ kk.abs().T).amax(1) * c
+            terms = (length + d + 64) * u
+            weights = pu.half_step(torch.bfloat16) if dtype == gk.BF16 else 0.0
+            bound = (w @ vv.abs()) * (weights + 4 * off + 4 * terms)[:, None] + want.abs() * pu.half_step(b.p.torch_dtype)
+            assert ((out[r0:r0 + n, h] - want).abs() <= bound).all(), (s, h)
+            assert ((lse[r0:r0 + n, h] - want_lse).abs() <= 2 * off + 2 * terms + want_lse.abs() * 8 * u).all(), (s, h)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_over_the_longest_tables(dtype):
     """Tables of 2^30 tokens with more heads and sequences than the kernel for few rows would count, which takes none of them."""
