@@ -290,13 +290,15 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
  * are cut to 0 .. table_pages * page_tokens, row numbers to 0 .. n_rows and to
  * max_rows a sequence.  A position whose page number is not one of 0 .. n_pages-1, and
  * a row whose position is negative (more rows than tokens), has no place: it is not
- * written, it reads as zeros, nothing sees it.
+ * written, it reads as zeros, nothing sees it.  (Where row numbers do not ascend, a row that
+ * several sequences would take gets what any of them gives it, or parts of each.)
  *
  * 8-bit forms keep a row of a head with one scale: the least power of two 2^k with
  * max|x| <= 448 * 2^k and codes in e4m3 (OCP, no infinities), or max|x| / 127 rounded
  * to 32 bits and integer codes; codes are the values nearest to x / scale, ties to the even
  * one.  Rows with max|x| < 2^-100 have scale and codes 0.  Infinities and NaN in rows
- * to be written are not supported with them.
+ * to be written are not supported with them; magnitudes beyond 1.9 * 2^127 may come back as
+ * infinities, since the nearest code may stand for 2^128.
  */
 enum { GRAPHKV_PAGES_PLAIN = 0, GRAPHKV_PAGES_FP8 = 1, GRAPHKV_PAGES_INT8 = 2 };
 
@@ -311,7 +313,8 @@ typedef struct graphkv_paged_params {
     int32_t n_seqs;        /* 0 .. 2^20                                                  */
     int32_t table_pages;   /* >= 1, table_pages * page_tokens <= 2^30                    */
     int32_t n_rows;        /* rows of the row tensors, 0 .. 2^24 - 1                     */
-    int32_t max_rows;      /* no sequence has more rows than this; 0: n_rows             */
+    int32_t max_rows;      /* no sequence has more rows than this; 0: n_rows.  Tell it:  */
+                           /*   attend chooses its kernels by it (see there)             */
     float   softmax_scale; /* attend: 0 selects 1/sqrt(d), else in (0, 2^127]            */
     int32_t impl;          /* GRAPHKV_IMPL_*: GENERIC forces the scalar kernel (attend)  */
     int64_t row_stride;    /* elements between rows and between heads of K and V (write, */
@@ -351,6 +354,9 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  *        overlap
  *   lse  [n_rows, H_q]    out, optional (NULL), fp32
  *   ws   graphkv_attend_workspace_bytes(p) bytes, 256-byte aligned
+ * Sequences of few rows and of many have kernels of their own, and the host, which does not
+ * know the lengths, goes by max_rows: a step of single tokens that leaves it 0 is planned as
+ * one that may hold a chunk of n_rows, in blocks for many rows or with a launch that finds nothing.
  * Work is counted in 32 bits: where the matrix-core kernels run (AUTO, d up to 256 for bf16
  * and 128 for fp32), params are refused with n_rows * H_q / H_kv > 2^30, with n_rows * H_q + 192 *
  * n_seqs * H_kv >= 2^35, or, if some sequences may go to the kernel for few rows (max_rows * H_q / H_kv
@@ -360,8 +366,8 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  * Softmax statistics and sums are held in 32 bits.  With bf16 rows the weights (times the
  * values' scales, of 8-bit pages) are rounded to bf16 for the product with the values; where the kernel
  * for few rows reads plain pages, to two bf16 numbers each, which keep 16 bits.  (Sums of values
- * beyond 2^100 may leave the range of 32 bits.)  A row that sees nothing has
- * out = 0 and lse = -infinity.  What lies in places that a row does not see (later
+ * beyond 2^100 may leave the range of 32 bits.)  A row that sees nothing, or
+ * nothing but logits of -infinity, has out = 0 and lse = -infinity.  What lies in places that a row does not see (later
  * positions, the rest of a page) has no influence on it, whatever its bits.
  * Results are deterministic; a sequence's may differ in their last bits with the
  * sequences beside it, which change where its sums are cut.
@@ -387,7 +393,8 @@ const char *graphkv_strerror(int32_t code);
  * GRAPHKV_IMPL_AUTO, the matrix-core kernels that take their place; an update of the
  * scores that the next selection does first is counted with that selection, and so is
  * the gather of few rows behind it; a later round's bound and filter in one launch count
- * as cosine_bound_new.
+ * as cosine_bound_new.  attend_many counts both kernels for many rows, that for blocks of
+ * 256 and that for smaller ones.
  */
 enum {
     GRAPHKV_K_SCORE_STATS = 0, GRAPHKV_K_SCORE_VOTES, GRAPHKV_K_POOL, GRAPHKV_K_TOPK_SOURCES,

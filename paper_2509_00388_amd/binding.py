@@ -100,7 +100,9 @@ class _CPagedParams(ctypes.Structure):
 
 @dataclass
 class PagedParams:
-    """Mirror of graphkv_paged_params (see include/graphkv.h for the constraints); strides come from the tensors."""
+    """Mirror of graphkv_paged_params (see include/graphkv.h for the constraints); strides come from the tensors.
+    max_rows: no sequence has more new rows than this, 0 stands for n_rows.  graphkv_attend() chooses its kernels by it: a step of
+    single tokens says 1."""
     n_kv_heads: int
     head_dim: int
     page_tokens: int

@@ -383,6 +383,34 @@ def test_attention_of_rows_that_see_nothing(dtype, impl):
 
 @pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
 @pytest.mark.parametrize("dtype", TYPES)
+def test_attention_of_logits_of_minus_infinity(dtype, impl):
+    """Logits of -infinity weigh nothing; rows that see nothing else have zeros and -infinity, as rows that see nothing."""
+    say(f"logits of -infinity dtype={dtype} impl={impl}")
+    for pairs, G in (([(1, 300), (8, 90)], 4), ([(12, 300), (3, 40)], 4), ([(90, 400), (30, 60)], 4)):
+        b = pu.Batch(pairs, H=2, G=G, d=64, ps=16, dtype=dtype, impl=impl, before=1, behind=1)
+        Q = b.random_rows(2 * G)
+        Q[:, :, 7] = 1.5
+        for j in range(b.pairs[1][1]):
+            page, at = b.place(1, j)
+            b.pool["K"][page, :, at, 7] = -math.inf
+        n = pairs[0][1]
+        for j in list(range(0, n // 2)) + [n - 2]:
+            page, at = b.place(0, j)
+            b.pool["K"][page, :, at, 7] = -math.inf
+        out, lse = run_attend(b, Q)
+        r0, r1, r2 = b.start.tolist()
+        assert (out[r1:r2] == 0).all() and (lse[r1:r2] == -math.inf).all()
+        # the first sequence as if those keys were not there
+        kept = pu.Batch(pairs, H=2, G=G, d=64, ps=16, dtype=dtype, impl=impl, before=1, behind=1)
+        for name in "KV":
+            kept.pool[name] = b.pool[name]
+        cell = kept.place
+        kept.place = lambda s, pos: None if s == 1 or pos < n // 2 or pos == n - 2 else cell(s, pos)
+        pu.check_attend(kept, Q, out, lse)
+
+
+@pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_does_not_see_what_is_hidden(dtype, form, impl, d):
