@@ -376,8 +376,9 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
     // Sequences of few rows and of many go to different kernels where there are enough of both for two more launches: from eight
     // sequences on, unless the rows are as many as if all of them were as long as they may be (which the device alone knows: either
     // kernel for many rows takes any).  (A chunk of 500 rows beside steps over 2000 to 5000 tokens, eight key heads of four, us for one kernel
-    // / for both: plain pages, 3 steps 102 / 107, 7 106 / 113, 23 185 / 168, 127 561 / 436; fp8 pages 115 / 116, 124 / 115, 211 / 149,
-    // 690 / 304.  16 sequences of 64 rows each: 116 / 122.)
+    // / for both: plain pages, 3 steps 89 / 101, 7 105 / 113, 15 137 / 135, 23 168 / 158, 127 573 / 425; fp8 pages 99 / 106, 118 / 113, 154 / 128,
+    // 191 / 141, 676 / 288; int8 pages 97 / 102, 113 / 108, 150 / 124, 187 / 137, 645 / 291; plain fp32 449 / 455, 512 / 475, 641 / 528; plain pages of
+    // d = 64 67 / 70, 77 / 79, 102 / 92, of d = 256 214 / 244, 242 / 264, 297 / 305.  16 sequences of 64 rows each: 114 / 117, fp8 125 / 129.)
     A.many = (int64_t)b.max_rows * A.G > kFewRows;
     A.few = !A.many || (b.n_seqs >= 8 && (int64_t)b.n_seqs * b.max_rows > b.n_rows);
     if (A.few) {

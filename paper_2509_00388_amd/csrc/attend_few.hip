@@ -9,7 +9,7 @@
 //
 // Measured (bf16 rows, d = 128, eight key heads of four): one token over 131072 keys 97 us, 5.5 TB/s (reading alone is faster than the 4.6 of
 // a copy); 64 tokens over 400 to 5000 keys each in fp8 pages 93 us, 4.2 TB/s, where decode and the LDS share the time; one token
-// over 2048 keys 8.6 us, a chain of look-ups, loads, two products and the join of the waves with a tile a workgroup.  Slower: three workgroups
+// over 2048 keys 8.3 us, a chain of look-ups, loads, two products and the join of the waves with a tile a workgroup.  Slower: three workgroups
 // a compute unit, 768 or 1024 of them in all, 64 keys a wave.
 #include "attend_tile.hpp"
 #include "kernels.hpp"
