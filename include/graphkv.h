@@ -365,7 +365,7 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  * memory is needed: by the scalar kernel, and without rows or sequences.
  * Softmax statistics and sums are held in 32 bits.  With bf16 rows the weights (times the
  * values' scales, of 8-bit pages) are rounded to bf16 for the product with the values; where the kernel
- * for few rows reads plain pages, to two bf16 numbers each, which keep 16 bits.  (Sums of values
+ * for few rows reads plain pages, to two bf16 numbers each, which keep 15 bits.  (Sums of values
  * beyond 2^100 may leave the range of 32 bits.)  A row that sees nothing, or
  * nothing but logits of -infinity, has out = 0 and lse = -infinity.  What lies in places that a row does not see (later
  * positions, the rest of a page) has no influence on it, whatever its bits.

@@ -154,8 +154,8 @@ __device__ __forceinline__ void load_query(const T *row, int d, int hh, uint4 (&
 
 // A lane's weights of a block of 32 keys in bf16, as operands of two matrix steps.  The rounding, at most 2^-8 of a weight, is the price of
 // the bf16 matrix instruction: an output is off by about as much as by its own rounding to bf16.  Keeping what it leaves in a second
-// operand (add_values_twice()) makes it 2^-16 and doubles the product: us, one operand / two:
-//   attend_few   plain pages: a token over 131072 keys 105.6 / 105.9, 64 tokens 148.7 / 149.3, d = 64 84.0 / 85.2, d = 256 295.7 / 297.0
+// operand (add_values_twice()) makes it 2^-15 and doubles the product: us, one operand / two:
+//   attend_few   plain pages: a token over 131072 keys 105.9 / 106.1, 64 tokens 148.4 / 149.5, d = 64 84.9 / 85.6, d = 256 296.4 / 298.6
 //                fp8, int8 pages, 64 tokens: 97.3 / 99.5, 98.6 / 102; d = 64 63.9 / 66.6, 63.2 / 67
 //   attend_many  int8 drafts 49.4 / 51.8, seven chunks of 25 rows over 4000 keys 55.8 / 58.4
 //   attend_wide  2048 rows over 32768 keys 1080 / 1473
@@ -198,15 +198,19 @@ __device__ __forceinline__ void add_values(const unsigned char *vt, const float 
 {
     add_values<D, PITCH>(vt, pack_weights(p), lane, o);
 }
-// The same with what the rounding of the weights to bf16 leaves, as a second operand (p is used up).
+// The same with weights in two bf16 operands: the first cut off, the second what that leaves, at most 2^-7 of the weight and rounded by 2^-8 of
+// itself.  Where an infinite value meets them, both have to be above 0 (inf - inf, 0 x inf): the second is 2^-22 of the weight too large.
 template <int D, int PITCH>
-__device__ __forceinline__ void add_values_twice(const unsigned char *vt, float (&p)[16], int lane, f32x16 (&o)[D / 32])
+__device__ __forceinline__ void add_values_twice(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32])
 {
-    const Weights high = pack_weights(p);
+    float high[16], rest[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] -= (float)high.w[i >> 3][i & 7];   // (exact)
-    add_values<D, PITCH>(vt, high, lane, o);
-    add_values<D, PITCH>(vt, pack_weights(p), lane, o);
+    for (int i = 0; i < 16; ++i) {
+        high[i] = __uint_as_float(__float_as_uint(p[i]) & 0xffff0000u);
+        rest[i] = fmaf(p[i], 1.f + 0x1p-22f, -high[i]);
+    }
+    add_values<D, PITCH>(vt, pack_weights(high), lane, o);
+    add_values<D, PITCH>(vt, pack_weights(rest), lane, o);
 }
 template <int D, int PITCH>
 __device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], float)

@@ -7,7 +7,7 @@
 // read from the LDS some steps ahead, and the two waves of a SIMD fill one another's gaps.  The LDS holds three tiles: those two and the next,
 // which the waves write, from registers, while nobody reads it; one barrier a tile.
 // Measured (2048 rows of four query heads a key head over 32768 keys, eight key heads, d = 128, bf16; whole calls with their join of 10 us, one after
-// the other): 1045 to 1100 us from card to card, 975 to 1030 TFLOP/s while the kernel runs; on a card where it takes 1095 a library product of 8192
+// the other): 1020 to 1100 us from card to card, 975 to 1050 TFLOP/s while the kernel runs; on a card where it takes 1095 a library product of 8192
 // cubed reaches 1345, the kernel without its softmax took 850 us and without the reads of its operands from the LDS hardly less.  Slower, on one
 // card where the kernel took 1060 to 1095: 128 rows a workgroup and two of them 1290; a barrier between softmax and products that keeps the waves of a SIMD
 // half a tile apart 1090, with the operands' reads fixed by hand 1130, with tiles that pass the registers by (global_load_lds, pieces permuted

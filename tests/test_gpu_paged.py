@@ -383,6 +383,38 @@ def test_attention_of_rows_that_see_nothing(dtype, impl):
 
 @pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pairs,G,d", [([(1, 1)], 4, 64), ([(1, 300), (8, 90)], 4, 128), ([(1, 40), (2, 30)], 2, 256), ([(12, 300), (3, 40)], 4, 128),
+                                       ([(30, 200)], 4, 64), ([(90, 400), (30, 60)], 4, 128)])
+def test_attention_of_infinite_values(dtype, impl, pairs, G, d):
+    """Values that are infinite, at positions that all rows see and that some do: infinities of their sign in the rows that see them and
+    in no other place."""
+    say(f"infinite values dtype={dtype} impl={impl} {pairs} G={G} d={d}")
+    b = pu.Batch(pairs, H=2, G=G, d=d, ps=16, dtype=dtype, impl=impl, before=1, behind=1)
+    Q = b.random_rows(2 * G)
+    finite = b.pool["V"].clone()
+    odd = {}
+    for s, (n, length) in enumerate(pairs):
+        for j, column, sign in ((0, 3, 1), (length // 3, 20, -1), (length - 1 - n // 2, 40, 1)):
+            page, at = b.place(s, j)
+            b.pool["V"][page, :, at, column] = sign * math.inf
+            finite[page, :, at, column] = 0
+            odd[s, column] = (j, sign)
+    out, lse = run_attend(b, Q)
+    b.pool["V"] = finite
+    want, want_lse, bound, lse_bound = b.attend(Q)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    for r, s, pos in b.each_row():
+        rest = torch.ones(d, dtype=torch.bool)
+        for (owner, column), (j, sign) in odd.items():
+            if owner == s and j <= pos:
+                assert (out[r, :, column] == sign * math.inf).all(), (r, s, pos, column)
+                rest[column] = False
+        assert ((out[r] - want[r]).abs() <= bound[r] + 2.0 ** -100)[:, rest].all(), (r, s, pos)
+        assert ((lse[r] - want_lse[r]).abs() <= lse_bound[r]).all(), (r, s, pos)
+
+
+@pytest.mark.parametrize("impl", [gk.IMPL_AUTO, gk.IMPL_GENERIC])
+@pytest.mark.parametrize("dtype", TYPES)
 def test_attention_of_logits_of_minus_infinity(dtype, impl):
     """Logits of -infinity weigh nothing; rows that see nothing else have zeros and -infinity, as rows that see nothing."""
     say(f"logits of -infinity dtype={dtype} impl={impl}")
@@ -539,8 +571,9 @@ def test_attention_with_rising_logits(dtype, rise):
 
 @pytest.mark.parametrize("d", [64, 80, 128, 256])
 def test_attention_of_few_rows_keeps_the_weights(d):
-    """At most 32 stacked rows over plain pages in bf16: the weights go into the product with the values as two bf16 numbers each, so they
-    are off by half a step of the second, 2^-16 of the weight, not by 2^-8."""
+    """At most 32 stacked rows over plain pages in bf16: the weights go into the product with the values as two bf16 numbers each, the first
+    cut off, the second rounded: what the first leaves is at most 2^-7 of the weight, and half a step of that 2^-8 of it, so a weight is off by
+    2^-15 (and by the 2^-22 that the second is made larger by), not by 2^-8."""
     say(f"weights of few rows d={d}")
     b = pu.Batch([(1, 2), (1, 3), (1, 40), (2, 300), (8, 100), (3, 2), (1, 2000)], H=2, G=4, d=d, ps=16, before=1, behind=1, seed=d)
     Q = b.random_rows(8)
@@ -551,7 +584,7 @@ def test_attention_of_few_rows_keeps_the_weights(d):
     mass = b.attend(Q)[0]   # sums of the magnitudes
     b.pool["V"] = values
     mine = ~want.isnan()
-    allow = bound - (2.0 ** -8 - 2.0 ** -16) * mass
+    allow = bound - (2.0 ** -8 - 2.0 ** -15 - 2.0 ** -22) * mass
     assert ((out.cpu().double() - want).abs() <= allow + 2.0 ** -100)[mine].all()
 
 
