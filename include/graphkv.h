@@ -272,7 +272,8 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
  *   pools     [n_pages, H_kv, page_tokens, d], one for keys and one for values: rows
  *             of p->dtype (GRAPHKV_PAGES_PLAIN) or 8-bit codes (see below)
  *   scales    [n_pages, H_kv, page_tokens] fp32, of the codes: a row's values are its
- *             codes times its scale (NULL with GRAPHKV_PAGES_PLAIN)
+ *             codes times its scale (NULL with GRAPHKV_PAGES_PLAIN); with
+ *             GRAPHKV_PAGES_*_BLOCKS [n_pages, H_kv, page_tokens / scale_tokens]
  *   table     [n_seqs, table_pages] int32: entry i of sequence s is the page that holds
  *             its positions i * page_tokens and on
  *   seq_len   [n_seqs] int32: tokens of a sequence, new ones included
@@ -299,8 +300,18 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
  * one.  Rows with max|x| < 2^-100 have scale and codes 0.  Infinities and NaN in rows
  * to be written are not supported with them; magnitudes beyond 1.9 * 2^127 may come back as
  * infinities, since the nearest code may stand for 2^128.
+ *
+ * GRAPHKV_PAGES_FP8_BLOCKS and GRAPHKV_PAGES_INT8_BLOCKS keep a scale for each block of
+ * scale_tokens tokens of a head (positions that are next to one another, beginning at a multiple
+ * of scale_tokens): the same scale and codes, with max|x| over all rows of a block.  A block
+ * whose first token a call writes takes its scale from the rows of that call.  Rows that a call
+ * adds behind tokens which a block holds already keep the block's scale if it is as large as theirs would be;
+ * otherwise it becomes theirs, and the codes of the tokens before them become those nearest to code * old scale /
+ * new scale (for e4m3 the least bits of small values go, for integers each such step adds at most half of one of the new scale).
+ * A scale does not shrink while its block grows, not even where tokens that had asked for it were taken back.
  */
-enum { GRAPHKV_PAGES_PLAIN = 0, GRAPHKV_PAGES_FP8 = 1, GRAPHKV_PAGES_INT8 = 2 };
+enum { GRAPHKV_PAGES_PLAIN = 0, GRAPHKV_PAGES_FP8 = 1, GRAPHKV_PAGES_INT8 = 2,
+       GRAPHKV_PAGES_FP8_BLOCKS = 5, GRAPHKV_PAGES_INT8_BLOCKS = 6 };
 
 typedef struct graphkv_paged_params {
     int32_t n_kv_heads;    /* H_kv, 1 .. 65535                                           */
@@ -321,6 +332,8 @@ typedef struct graphkv_paged_params {
     int64_t head_stride;   /*   read) or Q (attend); both 0: packed [n_rows, heads, d].  */
     int64_t out_row_stride;   /* the same for the output of attend.  Strides are         */
     int64_t out_head_stride;  /*   multiples of 16 bytes, <= 2^38; output rows must not overlap */
+    int32_t scale_tokens;  /* with GRAPHKV_PAGES_*_BLOCKS: tokens that a scale belongs to, a */
+                           /*   power of two, 16 .. page_tokens (not read with other formats) */
 } graphkv_paged_params;
 
 /*
@@ -378,6 +391,50 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
                        const int32_t *seq_len, const int32_t *row_start, void *out, float *lse, void *ws,
                        size_t ws_bytes, void *stream);
 
+/*
+ * Attention of rows over all that another sequence holds (a decoder's rows over an encoder's states, or over anything
+ * that is no part of their own sequence): as graphkv_attend, but the rows of sequence s are no tokens of it, and each of
+ * them sees all positions 0 .. seq_len[s] - 1.  A sequence may have more rows than tokens; where seq_len[s] is 0, or
+ * none of its positions has a place, out = 0 and lse = -infinity.  The states are written once by graphkv_cache_write, in any page format.
+ *   ws   graphkv_attend_workspace_bytes(p) bytes, 256-byte aligned
+ */
+int32_t graphkv_cross_attend(const graphkv_paged_params *p, const void *Q, const void *Kpages, const void *Vpages,
+                             const float *Kscale, const float *Vscale, const int32_t *table, const int32_t *seq_len,
+                             const int32_t *row_start, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * What the calls above go by, made on the device: pages dealt to the sequences of a batch, their lengths and row
+ * numbers, and the place of each row.  One call serves all layers of a model, whose pools share a table.
+ *
+ * Sequence s, with len_before[s] tokens (cut to 0 .. table_pages * page_tokens), keeps the first keep[s] of them (cut to
+ * 0 .. that; keep = NULL: all) and gets new_rows[s] more (below 0: none).  It then needs more pages than it had, or fewer, and
+ * the rest go back.  Free pages are a stack: free_pages[0 .. n - 1] are free, n = free_before[0] (cut to 0 .. n_pages).
+ *   1. Refused are sequences with new_rows[s] > max_rows (n_rows if that is 0) or more tokens in the end than a table
+ *      holds, and then, in ascending order, those whose new rows, with the new rows of all sequences before them that are not
+ *      refused for these reasons, would be more than n_rows.
+ *   2. The pages that other sequences have too many go on the stack, those of the last sequence first, of each the last page first.
+ *   3. Sequences that need more pages take them from its top, in ascending order, for ascending entries of their table.  One that needs
+ *      more than are left is refused, and so is every later one that needs any.
+ * A refused sequence keeps its tokens and pages as they are and has no rows: seq_len[s] = len_before[s].  Others have
+ * seq_len[s] = kept + new.  new_rows[s] > 0 with row_start[s + 1] = row_start[s] tells a refusal.
+ *   seq_len     [n_seqs]              out, may be len_before
+ *   table       [n_seqs, table_pages] in/out: entries of pages that a sequence gets are written, no others
+ *   free_pages  [n_pages]             in/out
+ *   free_after  [1]                   out: how many are free then; may be free_before
+ *   row_start   [n_seqs + 1]          out: row_start[0] = 0, rows of refused sequences left out
+ *   positions   [n_rows]              out, optional (NULL): position of each row in its sequence, -1 from row_start[n_seqs] on
+ *   slots       [n_rows]              out, optional: page * page_tokens + place within it of each row, -1 likewise and
+ *                                     where a table names no page
+ *   ws          graphkv_assign_workspace_bytes(p) bytes, 256-byte aligned (0 up to 1024 sequences: it may be NULL)
+ * No other arrays may overlap.  Of the params, page_tokens, n_pages, n_seqs, table_pages, n_rows and max_rows are used, and all are
+ * checked.  A page belongs to one sequence or to the stack; where that is not so, pages may be lost or have two
+ * owners, but nothing outside the arrays is touched.
+ */
+size_t graphkv_assign_workspace_bytes(const graphkv_paged_params *p);
+int32_t graphkv_cache_assign(const graphkv_paged_params *p, const int32_t *keep, const int32_t *new_rows, const int32_t *len_before,
+                             int32_t *seq_len, int32_t *table, int32_t *free_pages, const int32_t *free_before, int32_t *free_after,
+                             int32_t *row_start, int32_t *positions, int32_t *slots, void *ws, size_t ws_bytes, void *stream);
+
 /* Host string for a return code (static storage). */
 const char *graphkv_strerror(int32_t code);
 
@@ -394,7 +451,8 @@ const char *graphkv_strerror(int32_t code);
  * scores that the next selection does first is counted with that selection, and so is
  * the gather of few rows behind it; a later round's bound and filter in one launch count
  * as cosine_bound_new.  attend_many counts both kernels for many rows, that for blocks of
- * 256 and that for smaller ones.
+ * 256 and that for smaller ones.  graphkv_cross_attend is counted with graphkv_attend, graphkv_cache_assign with
+ * cache_write.
  */
 enum {
     GRAPHKV_K_SCORE_STATS = 0, GRAPHKV_K_SCORE_VOTES, GRAPHKV_K_POOL, GRAPHKV_K_TOPK_SOURCES,

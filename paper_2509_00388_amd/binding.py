@@ -24,13 +24,15 @@ IMPL_AUTO, IMPL_GENERIC = 0, 1
 EDGES_KK, EDGES_KV, EDGES_VV = 0, 1, 2
 SCORER_ATTENTION, SCORER_KNORM = 0, 1
 PAGES_PLAIN, PAGES_FP8, PAGES_INT8 = 0, 1, 2
+PAGES_FP8_BLOCKS, PAGES_INT8_BLOCKS = 5, 6
 
 EXPORTS = ("graphkv_workspace_bytes", "graphkv_score", "graphkv_score_knorm", "graphkv_propagate",
            "graphkv_select", "graphkv_compress", "graphkv_strerror", "graphkv_uses_mfma",
            "graphkv_profile_begin", "graphkv_profile_end", "graphkv_kernel_name",
            "graphkv_workspace_bytes_batched", "graphkv_compress_batched", "graphkv_propagate_edges",
            "graphkv_compress_static", "graphkv_select_workspace_bytes", "graphkv_cache_write", "graphkv_cache_read",
-           "graphkv_attend", "graphkv_attend_workspace_bytes")
+           "graphkv_attend", "graphkv_attend_workspace_bytes", "graphkv_cross_attend", "graphkv_cache_assign",
+           "graphkv_assign_workspace_bytes")
 STATIC_SCRATCH_BYTES = 64 << 20
 N_KERNELS = 29
 
@@ -94,7 +96,7 @@ class _CPagedParams(ctypes.Structure):
         ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("table_pages", ctypes.c_int32),
         ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
         ("impl", ctypes.c_int32), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
-        ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64), ("scale_tokens", ctypes.c_int32),
     ]
 
 
@@ -102,7 +104,9 @@ class _CPagedParams(ctypes.Structure):
 class PagedParams:
     """Mirror of graphkv_paged_params (see include/graphkv.h for the constraints); strides come from the tensors.
     max_rows: no sequence has more new rows than this, 0 stands for n_rows.  graphkv_attend() chooses its kernels by it: a step of
-    single tokens says 1."""
+    single tokens says 1.
+    scale_tokens: tokens that a scale belongs to, with PAGES_FP8_BLOCKS and PAGES_INT8_BLOCKS; 0 stands for 32, or for
+    page_tokens where that is less."""
     n_kv_heads: int
     head_dim: int
     page_tokens: int
@@ -116,11 +120,12 @@ class PagedParams:
     page_format: int = PAGES_PLAIN
     softmax_scale: float = 0.0
     impl: int = IMPL_AUTO
+    scale_tokens: int = 0
 
     def c(self, rows=(0, 0), out=(0, 0)) -> _CPagedParams:
         return _CPagedParams(self.n_kv_heads, self.n_q_heads, self.head_dim, self.dtype, self.page_format, self.page_tokens,
                              self.n_pages, self.n_seqs, self.table_pages, self.n_rows, self.max_rows, self.softmax_scale,
-                             self.impl, *rows, *out)
+                             self.impl, *rows, *out, self.tokens_a_scale)
 
     @property
     def torch_dtype(self):
@@ -128,7 +133,16 @@ class PagedParams:
 
     @property
     def page_dtype(self):
-        return torch.float8_e4m3fn if self.page_format == PAGES_FP8 else torch.int8 if self.page_format == PAGES_INT8 else self.torch_dtype
+        f = self.page_format
+        return torch.float8_e4m3fn if f in (PAGES_FP8, PAGES_FP8_BLOCKS) else torch.int8 if f in (PAGES_INT8, PAGES_INT8_BLOCKS) else self.torch_dtype
+
+    @property
+    def in_blocks(self) -> bool:
+        return self.page_format in (PAGES_FP8_BLOCKS, PAGES_INT8_BLOCKS)
+
+    @property
+    def tokens_a_scale(self) -> int:
+        return (self.scale_tokens or min(32, self.page_tokens)) if self.in_blocks else 1
 
 
 _lib = None
@@ -178,6 +192,12 @@ def load_library() -> ctypes.CDLL:
     lib.graphkv_attend_workspace_bytes.argtypes = [gp]
     lib.graphkv_attend.restype = i32
     lib.graphkv_attend.argtypes = [gp] + [vp] * 11 + [sz, vp]
+    lib.graphkv_cross_attend.restype = i32
+    lib.graphkv_cross_attend.argtypes = [gp] + [vp] * 11 + [sz, vp]
+    lib.graphkv_assign_workspace_bytes.restype = sz
+    lib.graphkv_assign_workspace_bytes.argtypes = [gp]
+    lib.graphkv_cache_assign.restype = i32
+    lib.graphkv_cache_assign.argtypes = [gp] + [vp] * 12 + [sz, vp]
     lib.graphkv_strerror.restype = ctypes.c_char_p
     lib.graphkv_strerror.argtypes = [i32]
     lib.graphkv_profile_begin.restype = i32
@@ -442,8 +462,9 @@ def _pool_args(p: PagedParams, Kpages, Vpages, table, seq_len, row_start, Kscale
     dev, rows, dtype = Kpages.device, p.n_pages * p.n_kv_heads * p.page_tokens, p.page_dtype
     ks = vs = None
     if p.page_format != PAGES_PLAIN:
-        ks = _paged_arg(Kscale, "Kscale", torch.float32, rows, dev)
-        vs = _paged_arg(Vscale, "Vscale", torch.float32, rows, dev)
+        scales = rows // p.tokens_a_scale
+        ks = _paged_arg(Kscale, "Kscale", torch.float32, scales, dev)
+        vs = _paged_arg(Vscale, "Vscale", torch.float32, scales, dev)
     return (_paged_arg(Kpages, "Kpages", dtype, rows * p.head_dim, dev), _paged_arg(Vpages, "Vpages", dtype, rows * p.head_dim, dev),
             ks, vs, _paged_arg(table, "table", torch.int32, p.n_seqs * p.table_pages, dev),
             _paged_arg(seq_len, "seq_len", torch.int32, p.n_seqs, dev),
@@ -468,7 +489,8 @@ def _call_on(dev, f, *args):
 
 def graphkv_cache_write(p: PagedParams, K, V, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None):
     """Writes rows K, V [n_rows, H_kv, d] (views with strides are taken as they are) to the places of their tokens.
-    Kpages, Vpages [n_pages, H_kv, page_tokens, d] of p.page_dtype, scales [n_pages, H_kv, page_tokens] fp32."""
+    Kpages, Vpages [n_pages, H_kv, page_tokens, d] of p.page_dtype, scales [n_pages, H_kv, page_tokens] fp32, with pages in blocks
+    [n_pages, H_kv, page_tokens / scale_tokens]."""
     at, dev = _pool_args(p, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale)
     kp, ks = _rows_arg(p, K, "K", p.n_kv_heads, dev)
     vp, vs = _rows_arg(p, V, "V", p.n_kv_heads, dev)
@@ -499,10 +521,7 @@ def alloc_attend_workspace(p: PagedParams, device="cuda") -> torch.Tensor:
     return torch.empty(graphkv_attend_workspace_bytes(p), dtype=torch.uint8, device=device)
 
 
-def graphkv_attend(p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None, out=None,
-                   lse=None, ws=None):
-    """out [n_rows, H_q, d] (allocated if None): causal attention of the rows Q over their sequences' cached tokens.
-    lse: an fp32 tensor [n_rows, H_q] that gets the logarithms of the softmax sums."""
+def _attend(call: str, p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale, out, lse, ws):
     at, dev = _pool_args(p, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale)
     qp, qs = _rows_arg(p, Q, "Q", p.n_q_heads, dev)
     out = _new_rows(p, p.n_q_heads, dev) if out is None else out
@@ -512,8 +531,59 @@ def graphkv_attend(p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start,
     if ws is None:
         ws = torch.empty(load_library().graphkv_attend_workspace_bytes(ctypes.byref(cp)), dtype=torch.uint8, device=dev)
     wp = _paged_arg(ws, "ws", torch.uint8, 0, dev)
-    _check(_call_on(dev, load_library().graphkv_attend, ctypes.byref(cp), qp, *at, op, lp, wp, ws.numel()))
+    _check(_call_on(dev, getattr(load_library(), call), ctypes.byref(cp), qp, *at, op, lp, wp, ws.numel()))
     return out
+
+
+def graphkv_attend(p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None, out=None,
+                   lse=None, ws=None):
+    """out [n_rows, H_q, d] (allocated if None): causal attention of the rows Q over their sequences' cached tokens.
+    lse: an fp32 tensor [n_rows, H_q] that gets the logarithms of the softmax sums."""
+    return _attend("graphkv_attend", p, Q, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale, out, lse, ws)
+
+
+def graphkv_cross_attend(p: PagedParams, Q, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None, out=None,
+                         lse=None, ws=None):
+    """As graphkv_attend(), of rows that are no tokens of the sequences: each sees all seq_len[s] positions of sequence s."""
+    return _attend("graphkv_cross_attend", p, Q, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale, out, lse, ws)
+
+
+def graphkv_assign_workspace_bytes(p: PagedParams) -> int:
+    return int(load_library().graphkv_assign_workspace_bytes(ctypes.byref(p.c())))
+
+
+def alloc_assign_workspace(p: PagedParams, device="cuda") -> torch.Tensor:
+    return torch.empty(graphkv_assign_workspace_bytes(p), dtype=torch.uint8, device=device)
+
+
+def graphkv_cache_assign(p: PagedParams, new_rows, len_before, table, free_pages, free_before, keep=None, seq_len=None, free_after=None,
+                         row_start=None, positions=None, slots=None, ws=None):
+    """Deals pages to the sequences of a batch; all tensors int32 on one device.  Sequence s keeps keep[s] (None: all) of its
+    len_before[s] tokens and gets new_rows[s] more; table [n_seqs, table_pages] and the stack free_pages [n_pages], of which
+    free_before [1] are free, are updated.  Returns (seq_len [n_seqs], free_after [1], row_start [n_seqs + 1]), allocated where None;
+    seq_len and free_after may be len_before and free_before.  positions, slots: tensors [n_rows] that get the
+    position and the place in the pool of each row."""
+    if not isinstance(table, torch.Tensor) or not table.is_cuda:
+        raise GraphKVError("table must be a contiguous device tensor")
+    dev, n, lib = table.device, p.n_seqs, load_library()
+
+    def new(t, count):
+        return torch.empty(count, dtype=torch.int32, device=dev) if t is None else t
+    seq_len, free_after, row_start = new(seq_len, n), new(free_after, 1), new(row_start, n + 1)
+
+    def arg(t, name, count):
+        return _paged_arg(t, name, torch.int32, count, dev)
+    cp = p.c()
+    if ws is None and n > 1024:   # (fewer sequences use none)
+        ws = torch.empty(lib.graphkv_assign_workspace_bytes(ctypes.byref(cp)), dtype=torch.uint8, device=dev)
+    wp, wn = (None, 0) if ws is None else (_paged_arg(ws, "ws", torch.uint8, 0, dev), ws.numel())
+    _check(_call_on(dev, lib.graphkv_cache_assign, ctypes.byref(cp), None if keep is None else arg(keep, "keep", n),
+                    arg(new_rows, "new_rows", n), arg(len_before, "len_before", n), arg(seq_len, "seq_len", n),
+                    arg(table, "table", n * p.table_pages), arg(free_pages, "free_pages", p.n_pages), arg(free_before, "free_before", 1),
+                    arg(free_after, "free_after", 1), arg(row_start, "row_start", n + 1),
+                    None if positions is None else arg(positions, "positions", p.n_rows),
+                    None if slots is None else arg(slots, "slots", p.n_rows), wp, wn))
+    return seq_len, free_after, row_start
 
 
 def graphkv_profile_begin():

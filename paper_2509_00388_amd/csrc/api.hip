@@ -298,9 +298,11 @@ bool paged_ok(const graphkv_paged_params *p)
     if (!p) return false;
     if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return false;
     if (p->dtype != GRAPHKV_FP32 && p->dtype != GRAPHKV_BF16) return false;
-    if (p->page_format < GRAPHKV_PAGES_PLAIN || p->page_format > GRAPHKV_PAGES_INT8) return false;
+    const bool blocks = p->page_format == GRAPHKV_PAGES_FP8_BLOCKS || p->page_format == GRAPHKV_PAGES_INT8_BLOCKS;
+    if (!blocks && (p->page_format < GRAPHKV_PAGES_PLAIN || p->page_format > GRAPHKV_PAGES_INT8)) return false;
     if (p->head_dim < 8 || p->head_dim > 512 || p->head_dim % (p->page_format == GRAPHKV_PAGES_PLAIN ? 8 : 16)) return false;
     if (p->page_tokens < 1 || p->page_tokens > 65536 || (p->page_tokens & (p->page_tokens - 1))) return false;
+    if (blocks && (p->scale_tokens < 16 || p->scale_tokens > p->page_tokens || (p->scale_tokens & (p->scale_tokens - 1)))) return false;
     if (p->n_pages < 1 || (__int128)p->n_pages * p->n_kv_heads * p->page_tokens > INT32_MAX) return false;
     if (p->n_seqs < 0 || p->n_seqs > (1 << 20)) return false;
     if (p->table_pages < 1 || (int64_t)p->table_pages * p->page_tokens > (1 << 30)) return false;
@@ -339,6 +341,7 @@ PagedBatch batch_of(const graphkv_paged_params *p, const int32_t *table, const i
     b.H = p->n_kv_heads;
     b.d = p->head_dim;
     b.page_shift = __builtin_ctz((unsigned)p->page_tokens);
+    b.scale_shift = in_blocks(p->page_format) ? __builtin_ctz((unsigned)p->scale_tokens) : 0;
     return b;
 }
 
@@ -361,6 +364,8 @@ struct AttendPlan {
     ManyPlan mp;
     size_t few_slots, many_records, many_slots, total;   // places in the workspace
 };
+
+static_assert(kBlocksFp8 == GRAPHKV_PAGES_FP8_BLOCKS && kBlocksInt8 == GRAPHKV_PAGES_INT8_BLOCKS, "");
 
 bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
 {
@@ -405,6 +410,52 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
 }
 
 template <typename T> T *at(void *ws, size_t off) { return reinterpret_cast<T *>((char *)ws + off); }
+
+int32_t run_attend(const graphkv_paged_params *p, bool cross, const void *Q, const void *Kpages, const void *Vpages, const float *Kscale,
+                   const float *Vscale, const int32_t *table, const int32_t *seq_len, const int32_t *row_start, void *out, float *lse,
+                   void *ws, size_t ws_bytes, void *stream)
+{
+    AttendPlan A;
+    if (!plan_attend(p, A)) return GRAPHKV_EINVAL;
+    AttendArgs a{};
+    if (!take_strides(p, p->n_q_heads, p->row_stride, p->head_stride, false, a.q_row, a.q_head) ||
+        !take_strides(p, p->n_q_heads, p->out_row_stride, p->out_head_stride, true, a.o_row, a.o_head))
+        return GRAPHKV_EINVAL;
+    if (p->n_rows == 0 || p->n_seqs == 0) return GRAPHKV_OK;
+    if (!aligned16(Q) || !aligned16(out) || (lse && !aligned4(lse)) ||
+        !batch_pointers_ok(p, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start))
+        return GRAPHKV_EINVAL;
+    if (A.total)
+        if (int32_t rc = check_ws(A.total, ws, ws_bytes)) return rc;
+    a.b = batch_of(p, table, seq_len, row_start);
+    a.Q = Q;
+    a.Kpages = Kpages;
+    a.Vpages = Vpages;
+    a.Kscale = Kscale;
+    a.Vscale = Vscale;
+    a.out = out;
+    a.lse = lse;
+    a.G = A.G;
+    a.c = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
+    hipStream_t st = (hipStream_t)stream;
+    if (A.generic || cross || in_blocks(p->page_format)) {
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_GENERIC, launch_attend_generic(a, p->dtype, p->page_format, cross, st));
+        return GRAPHKV_OK;
+    }
+    if (A.few) {
+        A.fp.join.records = at<JoinRecord>(ws, 0);
+        A.fp.join.slots = at<float>(ws, A.few_slots);
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, st));
+    }
+    if (A.many) {
+        A.mp.join.records = at<JoinRecord>(ws, A.many_records);
+        A.mp.join.slots = at<float>(ws, A.many_slots);
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, st)
+                                                    : launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
+    }
+    GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, A.mp.join, p->dtype, st));
+    return GRAPHKV_OK;
+}
 
 int32_t run_score(const graphkv_params *p, const Dims &D, const Workspace &W, const void *Kc,
                   const void *Qw, float *scores, void *ws, hipStream_t st)
@@ -898,45 +949,54 @@ int32_t graphkv_attend(const graphkv_paged_params *p, const void *Q, const void 
                        const float *Kscale, const float *Vscale, const int32_t *table, const int32_t *seq_len,
                        const int32_t *row_start, void *out, float *lse, void *ws, size_t ws_bytes, void *stream)
 {
-    AttendPlan A;
-    if (!plan_attend(p, A)) return GRAPHKV_EINVAL;
-    AttendArgs a{};
-    if (!take_strides(p, p->n_q_heads, p->row_stride, p->head_stride, false, a.q_row, a.q_head) ||
-        !take_strides(p, p->n_q_heads, p->out_row_stride, p->out_head_stride, true, a.o_row, a.o_head))
+    return run_attend(p, false, Q, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start, out, lse, ws, ws_bytes, stream);
+}
+
+int32_t graphkv_cross_attend(const graphkv_paged_params *p, const void *Q, const void *Kpages, const void *Vpages,
+                             const float *Kscale, const float *Vscale, const int32_t *table, const int32_t *seq_len,
+                             const int32_t *row_start, void *out, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    return run_attend(p, true, Q, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start, out, lse, ws, ws_bytes, stream);
+}
+
+size_t graphkv_assign_workspace_bytes(const graphkv_paged_params *p)
+{
+    return paged_ok(p) ? align_up(assign_scratch_bytes(p->n_seqs)) : 0;
+}
+
+int32_t graphkv_cache_assign(const graphkv_paged_params *p, const int32_t *keep, const int32_t *new_rows, const int32_t *len_before,
+                             int32_t *seq_len, int32_t *table, int32_t *free_pages, const int32_t *free_before, int32_t *free_after,
+                             int32_t *row_start, int32_t *positions, int32_t *slots, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!paged_ok(p)) return GRAPHKV_EINVAL;
+    auto bad = [](const int32_t *ptr, bool needed) { return ptr ? ((uintptr_t)ptr & 3u) != 0 : needed; };
+    const bool any = p->n_seqs > 0;
+    if (bad(keep, false) || bad(new_rows, any) || bad(len_before, any) || bad(seq_len, any) || bad(table, any) || bad(free_pages, true) ||
+        bad(free_before, true) || bad(free_after, true) || bad(row_start, true) || bad(positions, false) || bad(slots, false))
         return GRAPHKV_EINVAL;
-    if (p->n_rows == 0 || p->n_seqs == 0) return GRAPHKV_OK;
-    if (!aligned16(Q) || !aligned16(out) || (lse && !aligned4(lse)) ||
-        !batch_pointers_ok(p, Kpages, Vpages, Kscale, Vscale, table, seq_len, row_start))
-        return GRAPHKV_EINVAL;
-    if (A.total)
-        if (int32_t rc = check_ws(A.total, ws, ws_bytes)) return rc;
-    a.b = batch_of(p, table, seq_len, row_start);
-    a.Q = Q;
-    a.Kpages = Kpages;
-    a.Vpages = Vpages;
-    a.Kscale = Kscale;
-    a.Vscale = Vscale;
-    a.out = out;
-    a.lse = lse;
-    a.G = A.G;
-    a.c = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
+    const size_t need = graphkv_assign_workspace_bytes(p);
+    if (need)
+        if (int32_t rc = check_ws(need, ws, ws_bytes)) return rc;
+    AssignArgs a{};
+    a.keep = keep;
+    a.new_rows = new_rows;
+    a.len_before = len_before;
+    a.free_before = free_before;
+    a.seq_len = seq_len;
+    a.table = table;
+    a.free_pages = free_pages;
+    a.free_after = free_after;
+    a.row_start = row_start;
+    a.positions = positions;
+    a.slots = slots;
+    a.n_seqs = p->n_seqs;
+    a.table_pages = p->table_pages;
+    a.n_pages = p->n_pages;
+    a.n_rows = p->n_rows;
+    a.max_rows = p->max_rows ? p->max_rows : p->n_rows;
+    a.page_shift = __builtin_ctz((unsigned)p->page_tokens);
     hipStream_t st = (hipStream_t)stream;
-    if (A.generic) {
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_GENERIC, launch_attend_generic(a, p->dtype, p->page_format, st));
-        return GRAPHKV_OK;
-    }
-    if (A.few) {
-        A.fp.join.records = at<JoinRecord>(ws, 0);
-        A.fp.join.slots = at<float>(ws, A.few_slots);
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, st));
-    }
-    if (A.many) {
-        A.mp.join.records = at<JoinRecord>(ws, A.many_records);
-        A.mp.join.slots = at<float>(ws, A.many_slots);
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, st)
-                                                    : launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
-    }
-    GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, A.mp.join, p->dtype, st));
+    GKV_LAUNCH(GRAPHKV_K_CACHE_WRITE, launch_assign(a, ws, st));
     return GRAPHKV_OK;
 }
 

@@ -1,0 +1,233 @@
+// Pages of a pool dealt to the sequences of a batch, and the numbers that the other calls go by (graphkv_cache_assign).
+//
+// A sequence with had tokens keeps some, gets new ones and then needs ceil(want / page) - ceil(had / page) pages: more, which
+// come from the top of a stack of free ones, or fewer, and then the rest go back to it.  Where in the stack, and from which row on
+// its rows lie, follows from sums over the sequences before it; who is refused follows from the same sums, since once the rows or
+// pages asked for pass what there is, they do so for all later sequences that ask for any.
+//
+//   asked  = sums of new rows                -> rows that do not fit are refused
+//   taken, given = sums of pages             -> pages beyond free + given are refused
+//   start  = sums of the rows that are left  -> row numbers
+//
+// Up to 1024 sequences a workgroup does all this, a sequence a thread, with three scans; beyond, workgroups of 1024 each go as far as they get
+// without the others' sums, leave theirs, and begin anew in the next launch: four of them, whatever the number.  Page numbers
+// and rows are dealt to the threads one by one, whoever's they are, and find their sequence in the sums, which lie in the LDS.  Few rows
+// are told their places in the same launch, many in one of their own.  Nothing but latency: a batch's numbers are a few kilobytes.
+#include "kernels.hpp"
+#include "paged.hpp"
+
+namespace gkv {
+
+namespace {
+
+constexpr int kChunk = 1024;        // sequences of a workgroup
+constexpr int kRowsAtOnce = 4096;   // rows that the workgroup tells their places itself
+
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Sums up to and with this thread's value, of NW waves; sums that pass 32 bits stay at the largest number.  `part`: 17 words.
+template <int NW> __device__ __forceinline__ uint32_t scan_sat(uint32_t v, uint32_t *part, uint32_t &total)
+{
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t incl = wave_scan_op(v, 0u, add_sat);
+    __syncthreads();   // (the scan before is done with `part`)
+    if (lane == kWave - 1) part[wv] = incl;
+    __syncthreads();
+    const uint32_t sums = wave_scan_op(lane < NW ? part[lane] : 0u, 0u, add_sat);
+    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, 63);
+    return add_sat(incl, wv > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, wv - 1) : 0u);
+}
+
+// The first of n ascending sums that is above i (n if none is).
+__device__ __forceinline__ int first_above(const uint32_t *sums, int n, uint32_t i)
+{
+    int lo = 0;
+    for (int len = n; len > 0;) {
+        const int half = len >> 1;
+        if (sums[lo + half] <= i) { lo += half + 1; len -= half + 1; }
+        else len = half;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ uint32_t pages_of(uint32_t tokens, int shift) { return (tokens + (1u << shift) - 1) >> shift; }
+
+// Place of a position in the pool (of head 0, in tokens), -1 if it has none.
+__device__ __forceinline__ int slot_of(const AssignArgs &a, int s, int pos)
+{
+    const int page = a.table[(long)s * a.table_pages + (pos >> a.page_shift)];
+    return (unsigned)page < (unsigned)a.n_pages ? (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : -1;
+}
+
+// Sums of the chunks before mine, of them all, of an array that the launch before left.
+template <int NW> __device__ __forceinline__ uint32_t chunks_before(const uint32_t *sums, int chunks, int mine, uint32_t *part, uint32_t &all)
+{
+    const int t = threadIdx.x;
+    scan_sat<NW>(t < mine ? sums[t] : 0u, part, all);
+    const uint32_t before = all;
+    scan_sat<NW>(t < chunks ? sums[t] : 0u, part, all);
+    return before;
+}
+
+// PHASE 0: all at once, a single chunk.  1 to 4: as far as the sums of the launches before allow (AssignSums).
+template <int NT, int PHASE>
+__global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sums)
+{
+    constexpr int NW = NT / kWave;
+    __shared__ uint32_t part[17], by_page[NT], by_row[NT];
+    __shared__ int first_entry[NT], length[NT];
+    const int t = threadIdx.x, chunk = blockIdx.x, s = chunk * NT + t, chunks = gridDim.x;
+    const bool mine = s < a.n_seqs;
+    const uint32_t cap = (uint32_t)a.table_pages << a.page_shift;
+
+    uint32_t had = 0, kept = 0, fresh = 0, n_free = 0;
+    if (mine) {
+        had = min((uint32_t)max(a.len_before[s], 0), cap);
+        kept = a.keep ? min((uint32_t)max(a.keep[s], 0), had) : had;
+        fresh = (uint32_t)max(a.new_rows[s], 0);
+    }
+    // (the numbers of free pages before and after may be one: phases beyond the first read what that one saw)
+    if (PHASE <= 1) n_free = (uint32_t)min(max(a.free_before[0], 0), a.n_pages);
+    else n_free = sums.n_free[0];
+    const uint32_t want = kept + fresh;   // (below 2^30 + 2^31)
+    const bool fits = fresh <= (uint32_t)a.max_rows && want <= cap;
+    if (!fits) fresh = 0;
+
+    uint32_t all, asked_before = 0, taken_before = 0, given_before = 0, start_before = 0, given_all;
+    if (PHASE >= 2) asked_before = chunks_before<NW>(sums.asked, chunks, chunk, part, all);
+    const uint32_t asked = add_sat(asked_before, scan_sat<NW>(fresh, part, all));
+    if (PHASE == 1) {
+        if (t == 0) sums.asked[chunk] = all;
+        if (t == 0 && chunk == 0) sums.n_free[0] = n_free;
+        return;
+    }
+    bool ok = fits && (fresh == 0 || asked <= (uint32_t)a.n_rows);
+    const uint32_t pages = pages_of(had, a.page_shift), after = pages_of(want, a.page_shift);
+    const uint32_t take = ok && after > pages ? after - pages : 0, give = ok && after < pages ? pages - after : 0;
+    uint32_t take_all;
+    uint32_t taken = scan_sat<NW>(take, part, take_all);
+    uint32_t given = scan_sat<NW>(give, part, given_all);
+    const uint32_t given_here = given_all;
+    if (PHASE == 2) {
+        if (t == 0) { sums.taken[chunk] = take_all; sums.given[chunk] = given_here; }
+        return;
+    }
+    if (PHASE >= 3) {
+        taken_before = chunks_before<NW>(sums.taken, chunks, chunk, part, all);
+        given_before = chunks_before<NW>(sums.given, chunks, chunk, part, given_all);
+    }
+    const uint32_t total = min(add_sat(n_free, given_all), (uint32_t)a.n_pages);   // (more only where a page has two owners)
+    ok = ok && (take == 0 || add_sat(taken_before, taken) <= total);
+
+    if (PHASE == 0 || PHASE == 3) {
+        // Pages that come back: number i of all to entry total - 1 - i, so that what was taken last lies on top again where a
+        // call undoes another.
+        if (given_here > 0) {
+            __syncthreads();
+            by_page[t] = given;
+            first_entry[t] = (int)after - (int)(given - give);
+            __syncthreads();
+            const uint32_t room = total - n_free > given_before ? total - n_free - given_before : 0;
+            for (uint32_t i = t; i < min(given_here, room); i += NT) {
+                const int owner = first_above(by_page, NT, i);
+                if (owner < NT)
+                    a.free_pages[total - 1 - (given_before + i)] = a.table[(long)(chunk * NT + owner) * a.table_pages + (first_entry[owner] + (int)i)];
+            }
+        }
+    }
+    const uint32_t rows = ok ? fresh : 0;
+    uint32_t rows_all, out_all;
+    const uint32_t rows_to = scan_sat<NW>(rows, part, rows_all);
+    scan_sat<NW>(ok ? take : 0, part, out_all);   // (those that are served come first: their sums are `taken`)
+    if (PHASE == 3) {
+        if (t == 0) { sums.rows[chunk] = rows_all; sums.out[chunk] = out_all; }
+        return;
+    }
+    uint32_t rows_total = rows_all, out_total = out_all;
+    if (PHASE == 4) {
+        start_before = chunks_before<NW>(sums.rows, chunks, chunk, part, rows_total);
+        chunks_before<NW>(sums.out, chunks, chunk, part, out_total);
+    }
+    const uint32_t len = ok ? want : had;
+    if (mine) {
+        a.seq_len[s] = (int32_t)len;
+        a.row_start[s] = (int32_t)(start_before + rows_to - rows);
+    }
+    if (t == 0 && chunk == 0) {
+        a.free_after[0] = (int32_t)(total - out_total);
+        a.row_start[a.n_seqs] = (int32_t)rows_total;
+    }
+    __syncthreads();   // (pages that came back may be dealt out again)
+    by_page[t] = taken;
+    by_row[t] = rows_to;
+    first_entry[t] = (int)pages - (int)(taken - take);
+    length[t] = (int)len;
+    __syncthreads();
+    for (uint32_t i = t; i < out_all; i += NT) {
+        const int owner = first_above(by_page, NT, i);
+        if (owner < NT)
+            a.table[(long)(chunk * NT + owner) * a.table_pages + (first_entry[owner] + (int)i)] = a.free_pages[total - 1 - (taken_before + i)];
+    }
+    if (PHASE == 0 && a.rows_here) {
+        __syncthreads();
+        for (int r = t; r < a.n_rows; r += NT) {
+            int pos = -1, slot = -1;
+            if (r < (int)rows_all) {
+                const int owner = first_above(by_row, NT, (uint32_t)r);
+                pos = length[owner] - (int)by_row[owner] + r;
+                slot = slot_of(a, owner, pos);
+            }
+            if (a.positions) a.positions[r] = pos;
+            if (a.slots) a.slots[r] = slot;
+        }
+    }
+}
+
+// Position and place of each row, a row a thread.
+__global__ __launch_bounds__(256) void assign_rows_kernel(AssignArgs a)
+{
+    const int r = blockIdx.x * 256 + threadIdx.x;
+    if (r >= a.n_rows) return;
+    int pos = -1, slot = -1;
+    if (r < a.row_start[a.n_seqs]) {
+        int lo = 0;   // the first sequence that ends behind the row
+        for (int len = a.n_seqs; len > 0;) {
+            const int half = len >> 1;
+            if (a.row_start[lo + half + 1] <= r) { lo += half + 1; len -= half + 1; }
+            else len = half;
+        }
+        pos = a.seq_len[lo] - a.row_start[lo + 1] + r;
+        slot = slot_of(a, lo, pos);
+    }
+    if (a.positions) a.positions[r] = pos;
+    if (a.slots) a.slots[r] = slot;
+}
+
+int chunks_of(int n_seqs) { return (n_seqs + kChunk - 1) / kChunk; }
+
+}  // namespace
+
+size_t assign_scratch_bytes(int n_seqs) { return n_seqs <= kChunk ? 0 : (size_t)(5 * chunks_of(n_seqs) + 1) * 4; }
+
+hipError_t launch_assign(const AssignArgs &args, void *scratch, hipStream_t st)
+{
+    AssignArgs a = args;
+    const bool maps = (a.positions || a.slots) && a.n_rows > 0;
+    const int chunks = chunks_of(a.n_seqs);
+    if (chunks <= 1) {
+        a.rows_here = maps && a.n_rows <= kRowsAtOnce;
+        if (a.n_seqs <= 256) assign_kernel<256, 0><<<1, 256, 0, st>>>(a, AssignSums{});
+        else assign_kernel<kChunk, 0><<<1, kChunk, 0, st>>>(a, AssignSums{});
+    } else {
+        uint32_t *w = reinterpret_cast<uint32_t *>(scratch);
+        const AssignSums sums{w, w + chunks, w + 2 * chunks, w + 3 * chunks, w + 4 * chunks, w + 5 * chunks};
+        assign_kernel<kChunk, 1><<<chunks, kChunk, 0, st>>>(a, sums);
+        assign_kernel<kChunk, 2><<<chunks, kChunk, 0, st>>>(a, sums);
+        assign_kernel<kChunk, 3><<<chunks, kChunk, 0, st>>>(a, sums);
+        assign_kernel<kChunk, 4><<<chunks, kChunk, 0, st>>>(a, sums);
+    }
+    if (maps && !a.rows_here) assign_rows_kernel<<<(a.n_rows + 255) / 256, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace gkv

@@ -16,8 +16,8 @@ namespace {
 __device__ __forceinline__ void put(float *p, float x) { *p = x; }
 __device__ __forceinline__ void put(uint16_t *p, float x) { *p = (uint16_t)pack_bf16(x, 0.f); }
 
-template <typename T, int FORM>
-__global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
+template <typename T, int FORM, bool CROSS>
+__device__ __forceinline__ void attend_row(const AttendArgs &a)
 {
     using C = Cached<T, FORM>;
     __shared__ float q[512], p[256], red[16];
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
     if (s >= a.b.n_seqs) return;
     const SeqRows sq = seq_rows(a.b, s);
     if (row < sq.row0 || row >= sq.row0 + sq.n) return;
-    const int seen = max(0, sq.len - sq.n + (row - sq.row0) + 1);   // keys 0 .. seen - 1
+    const int seen = CROSS ? sq.len : max(0, sq.len - sq.n + (row - sq.row0) + 1);   // keys 0 .. seen - 1
     const T *qr = reinterpret_cast<const T *>(a.Q) + row * a.q_row + hq * a.q_head;
     for (int i = tid; i < d; i += 256) q[i] = to_float(qr[i]);
     float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
@@ -45,13 +45,13 @@ __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
 #pragma unroll
                 for (int e = 0; e < C::kPerVec; ++e) dot = fmaf(q[i + e], v[e], dot);
             }
-            x = dot * a.c * (FORM == kPagesPlain ? 1.f : a.Kscale[r]);
+            x = dot * a.c * (FORM == kPagesPlain ? 1.f : a.Kscale[scale_of_row<FORM>(a.b, r)]);
         }
         const float top = fmaxf(m, block_max(x, red));
         const float shift = top == -INFINITY ? 0.f : top;   // (nothing seen yet: all terms are 2^-inf)
         const float w = exp2f(x - shift), fade = exp2f(m - shift);
         at[tid] = r;
-        p[tid] = FORM == kPagesPlain || r < 0 ? w : w * a.Vscale[r];
+        p[tid] = FORM == kPagesPlain || r < 0 ? w : w * a.Vscale[scale_of_row<FORM>(a.b, r)];
         l = l * fade + block_sum(w, red);
         m = top;
         __syncthreads();
@@ -72,6 +72,11 @@ __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a)
         if (tid + 256 * u < d) put(out + tid + 256 * u, acc[u] * inverse_of(l));
     if (a.lse && tid == 0) a.lse[(long)row * a.b.H * a.G + hq] = lse_of(m, l);
 }
+
+template <typename T, int FORM> __global__ __launch_bounds__(256) void attend_generic_kernel(AttendArgs a) { attend_row<T, FORM, false>(a); }
+// (pages in blocks; rows that see all of a sequence)
+template <typename T, int FORM> __global__ __launch_bounds__(256) void blocks_scalar_kernel(AttendArgs a) { attend_row<T, FORM, false>(a); }
+template <typename T, int FORM> __global__ __launch_bounds__(256) void cross_scalar_kernel(AttendArgs a) { attend_row<T, FORM, true>(a); }
 
 // The parts of blocks of rows that several workgroups hold, put together: workgroup (y, w) takes rows y * rows_per_wg and on of the
 // block whose first part workgroup w of the kernel for few rows, or behind those of the one for many, held (in this order, so that the few w that hold one spread over all XCDs).  A row is 256 / GROUPS lanes wide, four sums a lane; where the parts are many, several
@@ -154,15 +159,16 @@ hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &few, const Jo
     return D == 64 ? go(attend_join_kernel<uint16_t, 64>) : D == 128 ? go(attend_join_kernel<uint16_t, 128>) : go(attend_join_kernel<uint16_t, 256>);
 }
 
-hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st)
+hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, bool cross, hipStream_t st)
 {
     const dim3 grid(a.b.n_rows, a.b.H * a.G);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); return hipGetLastError(); };
-    if (dtype == 0)
-        return form == kPagesPlain ? go(attend_generic_kernel<float, kPagesPlain>)
-             : form == kPagesFp8   ? go(attend_generic_kernel<float, kPagesFp8>) : go(attend_generic_kernel<float, kPagesInt8>);
-    return form == kPagesPlain ? go(attend_generic_kernel<uint16_t, kPagesPlain>)
-         : form == kPagesFp8   ? go(attend_generic_kernel<uint16_t, kPagesFp8>) : go(attend_generic_kernel<uint16_t, kPagesInt8>);
+    return with_form(form, [&](auto f) {
+        constexpr int FORM = decltype(f)::value;
+        auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); return hipGetLastError(); };
+        if (cross) return dtype == 0 ? go(cross_scalar_kernel<float, FORM>) : go(cross_scalar_kernel<uint16_t, FORM>);
+        if constexpr (in_blocks(FORM)) return dtype == 0 ? go(blocks_scalar_kernel<float, FORM>) : go(blocks_scalar_kernel<uint16_t, FORM>);
+        else return dtype == 0 ? go(attend_generic_kernel<float, FORM>) : go(attend_generic_kernel<uint16_t, FORM>);
+    });
 }
 
 }  // namespace gkv

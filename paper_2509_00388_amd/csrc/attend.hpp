@@ -186,7 +186,7 @@ __device__ __forceinline__ bool next_part(const AttendArgs &a, const ManyPlan &p
 bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
 ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);   // no workgroups: more units than 31 bits count
-hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, hipStream_t st);
+hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, bool cross, hipStream_t st);
 hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
 hipError_t launch_attend_wide(const AttendArgs &a, const ManyPlan &pl, int form, hipStream_t st);

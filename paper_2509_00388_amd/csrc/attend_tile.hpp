@@ -316,11 +316,11 @@ __device__ __forceinline__ float to_float(uint16_t x) { return bf16_to_f32(x); }
 // A value of a cached row.
 template <typename T, int FORM> __device__ __forceinline__ float cached_value(const void *rows, long at)
 {
-    if constexpr (FORM == kPagesFp8) {
+    if constexpr (code_of(FORM) == kPagesFp8) {
         float o[4];
         decode4<kPagesFp8>(reinterpret_cast<const uint8_t *>(rows)[at], o);
         return o[0];
-    } else if constexpr (FORM == kPagesInt8) {
+    } else if constexpr (code_of(FORM) == kPagesInt8) {
         return (float)reinterpret_cast<const int8_t *>(rows)[at];
     } else if constexpr (sizeof(T) == 2) {
         return bf16_to_f32(reinterpret_cast<const uint16_t *>(rows)[at]);

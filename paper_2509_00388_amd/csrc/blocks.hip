@@ -1,0 +1,176 @@
+// Rows written to pages of 8-bit codes with a scale for each block of tokens of a head (graphkv_cache_write).
+//
+// The scale of a block is that of its largest magnitude, so rows of a block are encoded together.  Rows that a call adds to
+// a block which holds earlier tokens keep its scale if it is enough for them; otherwise the scale grows to theirs, and the codes that are there are
+// rounded again, round(code * old / new): a power of two apart for e4m3, in 64 bits for integers.
+//
+// A workgroup takes a block of a head: the largest magnitude of its new rows, then their codes; rows stay in registers between the two where they
+// are few enough, else they are read again.  Blocks are found by their first new row: a workgroup looks at a stretch of rows for those that
+// begin one.
+#include "kernels.hpp"
+#include "paged.hpp"
+
+namespace gkv {
+
+namespace {
+
+constexpr int kHeld = 4;   // pieces of each tensor that a thread keeps between its two passes
+
+// Codes 0 .. 15 of a piece, to the scale `after`.
+template <int FORM> __device__ __forceinline__ uint4 encode_again(const uint4 &v, float before, float after)
+{
+    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+    uint32_t out[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x[4];
+        decode4<FORM>(in[i], x);
+        if (code_of(FORM) == kPagesFp8) {
+            out[i] = encode4<FORM>(x, after, before / after);   // (a power of two, or 0 where the codes become zeros)
+        } else {
+            out[i] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[i] |= (uint32_t)((int)rint((double)x[e] * (double)before / (double)after) & 0xff) << (8 * e);
+        }
+    }
+    return make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+// What a thread has of a block's new rows of one tensor: rows first + t * step, a piece of 16 bytes each.
+template <typename T> __device__ __forceinline__ float largest_of(const uint4 &v, float a)
+{
+    float x[Elem<T>::kPerVec];
+    Elem<T>::unpack(v, x);
+#pragma unroll
+    for (int e = 0; e < Elem<T>::kPerVec; ++e) a = fmaxf(a, fabsf(x[e]));
+    return a;
+}
+template <typename T, int FORM> __device__ __forceinline__ void put_codes(char *to, const uint4 &v, float s, float inv)
+{
+    constexpr int PER = Elem<T>::kPerVec;
+    float x[PER];
+    uint32_t w[PER / 4];
+    Elem<T>::unpack(v, x);
+#pragma unroll
+    for (int e = 0; e < PER; e += 4) w[e / 4] = s > 0.f ? encode4<FORM>(x + e, s, inv) : 0u;
+    if constexpr (PER == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t *>(to) = w[0];
+}
+
+struct BlocksWrite {
+    const void *K, *V;
+    long row_stride, head_stride;
+    void *Kpages, *Vpages;
+    float *Kscale, *Vscale;
+    int group, stretch;   // lanes of a row, rows that a workgroup looks at
+};
+
+template <typename T, int FORM>
+__global__ __launch_bounds__(256) void blocks_write_kernel(PagedBatch b, BlocksWrite w)
+{
+    constexpr int PER = Elem<T>::kPerVec;
+    __shared__ float tops[2][4];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, h = blockIdx.y;
+    const int at = tid & (w.group - 1), mine = tid / w.group, step = 256 / w.group, pieces = b.d / PER;
+    const int tokens = 1 << b.scale_shift;
+    const T *K = reinterpret_cast<const T *>(w.K) + h * w.head_stride, *V = reinterpret_cast<const T *>(w.V) + h * w.head_stride;
+
+    const int last = min((int)(blockIdx.x + 1) * w.stretch, b.n_rows);
+    for (int row = blockIdx.x * w.stretch; row < last;) {
+        const int s = seq_of_row(b, row, lane);
+        if (s >= b.n_seqs) break;
+        const SeqRows q = seq_rows(b, s);
+        const int i = row - q.row0, pos = q.len - q.n + i;
+        if (i < 0 || i >= q.n) { ++row; continue; }
+        if (pos < 0) { row += min(-pos, q.n - i); continue; }
+        const int inside = pos & (tokens - 1);
+        const int rest = min(tokens - inside, q.len - pos);   // rows up to the block's end or the sequence's
+        if (inside > 0 && i > 0 && pos > 0) { row += rest; continue; }   // the block's first new row is another's
+        const int first = row, page = page_of(b, s, pos);
+        row += rest;
+        if (page < 0) continue;
+
+        const int base = pool_row(b, page, h, pos - inside), block = base >> b.scale_shift;
+        const bool held = rest <= kHeld * step && pieces <= w.group;
+        uint4 kv[kHeld], vv[kHeld];
+        float ka = 0.f, va = 0.f;
+        auto row_of = [&](const T *x, int r) { return reinterpret_cast<const uint4 *>(x + (first + r) * w.row_stride); };
+        if (held) {
+#pragma unroll
+            for (int t = 0; t < kHeld; ++t) {
+                const int r = mine + t * step;
+                const bool in = at < pieces && r < rest;
+                kv[t] = in ? row_of(K, r)[at] : make_uint4(0, 0, 0, 0);
+                vv[t] = in ? row_of(V, r)[at] : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int t = 0; t < kHeld; ++t) {
+                ka = largest_of<T>(kv[t], ka);
+                va = largest_of<T>(vv[t], va);
+            }
+        } else {
+            for (int r = mine; r < rest; r += step)
+                for (int p = at; p < pieces; p += w.group) {
+                    ka = largest_of<T>(row_of(K, r)[p], ka);
+                    va = largest_of<T>(row_of(V, r)[p], va);
+                }
+        }
+        const float kb = inside > 0 ? w.Kscale[block] : 0.f, vb = inside > 0 ? w.Vscale[block] : 0.f;
+        ka = wave_max(ka);
+        va = wave_max(va);
+        __syncthreads();   // (the block before is done with them)
+        if (lane == 0) { tops[0][wv] = ka; tops[1][wv] = va; }
+        __syncthreads();
+        ka = fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3]));
+        va = fmaxf(fmaxf(tops[1][0], tops[1][1]), fmaxf(tops[1][2], tops[1][3]));
+        const float ks = fmaxf(kb, scale_of<FORM>(ka)), vs = fmaxf(vb, scale_of<FORM>(va));
+        const float kinv = ks > 0.f ? 1.f / ks : 0.f, vinv = vs > 0.f ? 1.f / vs : 0.f;
+        if (tid == 0) { w.Kscale[block] = ks; w.Vscale[block] = vs; }
+        char *kto = reinterpret_cast<char *>(w.Kpages) + (long)base * b.d, *vto = reinterpret_cast<char *>(w.Vpages) + (long)base * b.d;
+        if (kb < ks || vb < vs) {
+            const int old = inside * (b.d / 16);   // (the codes before the first new row are a run of them)
+            for (int p = tid; p < old; p += 256) {
+                if (kb < ks) { uint4 *x = reinterpret_cast<uint4 *>(kto) + p; *x = encode_again<FORM>(*x, kb, ks); }
+                if (vb < vs) { uint4 *x = reinterpret_cast<uint4 *>(vto) + p; *x = encode_again<FORM>(*x, vb, vs); }
+            }
+        }
+        kto += (long)inside * b.d;
+        vto += (long)inside * b.d;
+        if (held) {
+#pragma unroll
+            for (int t = 0; t < kHeld; ++t) {
+                const int r = mine + t * step;
+                if (at >= pieces || r >= rest) continue;
+                put_codes<T, FORM>(kto + (long)r * b.d + at * PER, kv[t], ks, kinv);
+                put_codes<T, FORM>(vto + (long)r * b.d + at * PER, vv[t], vs, vinv);
+            }
+        } else {
+            for (int r = mine; r < rest; r += step)
+                for (int p = at; p < pieces; p += w.group) {
+                    put_codes<T, FORM>(kto + (long)r * b.d + p * PER, row_of(K, r)[p], ks, kinv);
+                    put_codes<T, FORM>(vto + (long)r * b.d + p * PER, row_of(V, r)[p], vs, vinv);
+                }
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_blocks_write(const PagedBatch &b, int dtype, int form, const void *K, const void *V, long row_stride,
+                               long head_stride, void *Kpages, void *Vpages, float *Kscale, float *Vscale, hipStream_t st)
+{
+    const int pieces = b.d / (dtype == 0 ? 4 : 8);
+    int group = 1;
+    while (group < pieces && group < kWave) group <<= 1;
+    // Stretches of a block's tokens, in which a long sequence begins one block; where sequences have fewer rows than that, or the rows are few
+    // altogether, a row each.
+    const int tokens = 1 << b.scale_shift;
+    const bool single = b.max_rows < tokens || (long)b.n_rows * b.H <= 4096;
+    const BlocksWrite w{K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, group, single ? 1 : tokens};
+    const dim3 grid((b.n_rows + w.stretch - 1) / w.stretch, b.H);
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(b, w); return hipGetLastError(); };
+    if (dtype == 0) return form == kBlocksFp8 ? go(blocks_write_kernel<float, kBlocksFp8>) : go(blocks_write_kernel<float, kBlocksInt8>);
+    return form == kBlocksFp8 ? go(blocks_write_kernel<uint16_t, kBlocksFp8>) : go(blocks_write_kernel<uint16_t, kBlocksInt8>);
+}
+
+}  // namespace gkv

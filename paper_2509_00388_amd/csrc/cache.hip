@@ -13,43 +13,6 @@ namespace gkv {
 
 namespace {
 
-// Rows whose largest magnitude is below this are stored as zeros: the quotients by their scale would leave the range of
-// normal 32-bit numbers.
-constexpr float kLeastMax = 0x1p-100f;
-
-// The scale that brings the largest magnitude a to the largest code.  fp8: the least power of two 2^k with a <= 448 * 2^k
-// (a code's precision does not depend on its size, so a power of two costs none, and the division by it is exact);
-// int8: a / 127.  0 for rows that are stored as zeros.
-template <int FORM> __device__ __forceinline__ float scale_of(float a)
-{
-    if (!(a >= kLeastMax)) return 0.f;
-    if (FORM == kPagesInt8) return a / 127.f;
-    const uint32_t u = __float_as_uint(a);   // a = (1 + mantissa) * 2^(exponent - 127), 448 = 1.75 * 2^8
-    return __uint_as_float(((u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0)) << 23);
-}
-
-// Nearest integer to x / s, ties to the even one, by the real quotient: the product with the reciprocal is at most one
-// step off, and x - q s is a number of 24 bits, so that comparing it with s / 2 is exact.
-__device__ __forceinline__ int int8_code(float x, float s, float inv)
-{
-    float q = rintf(x * inv);
-    const float r = fmaf(-q, s, x), half = 0.5f * s;
-    if (fabsf(r) > half || (fabsf(r) == half && ((int)q & 1))) q += copysignf(1.f, r);
-    return (int)fminf(fmaxf(q, -127.f), 127.f);
-}
-
-template <int FORM> __device__ __forceinline__ uint32_t encode4(const float *x, float s, float inv)
-{
-    if (FORM == kPagesFp8) {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
-        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w, true);
-    }
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w |= (uint32_t)(int8_code(x[e], s, inv) & 0xff) << (8 * e);
-    return w;
-}
-
 // One tensor's values of a (row, head), TURNS pieces a lane, encoded and stored.
 template <typename T, int FORM, int TURNS>
 __device__ __forceinline__ void store_row(const uint4 (&v)[TURNS], int pieces, int at, int group, long row, void *pages,
@@ -149,7 +112,7 @@ __device__ __forceinline__ void restore(const uint4 &v, float s, T *to)
         Cached<T, FORM>::unpack(v, x);
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] *= s;
-        if constexpr (FORM == kPagesInt8 && sizeof(T) == 2) {
+        if constexpr (code_of(FORM) == kPagesInt8 && sizeof(T) == 2) {
             bool middle = false;
 #pragma unroll
             for (int e = 0; e < 16; ++e) middle |= (__float_as_uint(x[e]) & 0xffffu) == 0x8000u;
@@ -164,10 +127,9 @@ __device__ __forceinline__ void restore(const uint4 &v, float s, T *to)
 }
 
 template <typename T, int FORM>
-__global__ __launch_bounds__(256) void cache_read_kernel(PagedBatch b, const void *__restrict__ Kpages,
-                                                         const void *__restrict__ Vpages, const float *__restrict__ Kscale,
-                                                         const float *__restrict__ Vscale, T *K, T *V, long row_stride,
-                                                         long head_stride, int group)
+__device__ __forceinline__ void read_row(const PagedBatch &b, const void *__restrict__ Kpages, const void *__restrict__ Vpages,
+                                         const float *__restrict__ Kscale, const float *__restrict__ Vscale, T *K, T *V, long row_stride,
+                                         long head_stride, int group)
 {
     using C = Cached<T, FORM>;
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -186,8 +148,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(PagedBatch b, const voi
             uint4 vv = reinterpret_cast<const uint4 *>(Vpages)[from * pieces + p];
             float ks = 1.f, vs = 1.f;
             if (FORM != kPagesPlain) {
-                ks = Kscale[from];
-                vs = Vscale[from];
+                ks = Kscale[scale_of_row<FORM>(b, (int)from)];
+                vs = Vscale[scale_of_row<FORM>(b, (int)from)];
             }
             if (page < 0) {   // a row that has no place reads as zeros
                 kv = vv = make_uint4(0, 0, 0, 0);
@@ -198,6 +160,24 @@ __global__ __launch_bounds__(256) void cache_read_kernel(PagedBatch b, const voi
             restore<T, FORM>(vv, vs, V + to);
         }
     }
+}
+
+template <typename T, int FORM>
+__global__ __launch_bounds__(256) void cache_read_kernel(PagedBatch b, const void *__restrict__ Kpages,
+                                                         const void *__restrict__ Vpages, const float *__restrict__ Kscale,
+                                                         const float *__restrict__ Vscale, T *K, T *V, long row_stride,
+                                                         long head_stride, int group)
+{
+    read_row<T, FORM>(b, Kpages, Vpages, Kscale, Vscale, K, V, row_stride, head_stride, group);
+}
+// (pages in blocks)
+template <typename T, int FORM>
+__global__ __launch_bounds__(256) void blocks_read_kernel(PagedBatch b, const void *__restrict__ Kpages,
+                                                          const void *__restrict__ Vpages, const float *__restrict__ Kscale,
+                                                          const float *__restrict__ Vscale, T *K, T *V, long row_stride,
+                                                          long head_stride, int group)
+{
+    read_row<T, FORM>(b, Kpages, Vpages, Kscale, Vscale, K, V, row_stride, head_stride, group);
 }
 
 // Lanes that take a (row, head) of so many pieces.
@@ -238,6 +218,7 @@ hipError_t launch_cache_write(const PagedBatch &b, int dtype, int form, const vo
                               long head_stride, void *Kpages, void *Vpages, float *Kscale, float *Vscale, hipStream_t st)
 {
     auto go = [&](auto f) { return f(b, K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, st); };
+    if (in_blocks(form)) return launch_blocks_write(b, dtype, form, K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, st);
     if (dtype == 0)
         return form == kPagesPlain ? go(write_rows<float, kPagesPlain>)
              : form == kPagesFp8   ? go(write_rows<float, kPagesFp8>) : go(write_rows<float, kPagesInt8>);
@@ -250,21 +231,23 @@ static hipError_t read_rows(const PagedBatch &b, const void *Kpages, const void 
                             const float *Vscale, void *K, void *V, long row_stride, long head_stride, hipStream_t st)
 {
     const int group = lanes_for(b.d / Cached<T, FORM>::kPerVec);
-    cache_read_kernel<T, FORM><<<turns_grid(b, group), 256, 0, st>>>(b, Kpages, Vpages, Kscale, Vscale, (T *)K, (T *)V,
-                                                                        row_stride, head_stride, group);
-    return hipGetLastError();
+    auto go = [&](auto kernel) {
+        kernel<<<turns_grid(b, group), 256, 0, st>>>(b, Kpages, Vpages, Kscale, Vscale, (T *)K, (T *)V, row_stride, head_stride, group);
+        return hipGetLastError();
+    };
+    if constexpr (in_blocks(FORM)) return go(blocks_read_kernel<T, FORM>);
+    else return go(cache_read_kernel<T, FORM>);
 }
 
 hipError_t launch_cache_read(const PagedBatch &b, int dtype, int form, const void *Kpages, const void *Vpages,
                              const float *Kscale, const float *Vscale, void *K, void *V, long row_stride, long head_stride,
                              hipStream_t st)
 {
-    auto go = [&](auto f) { return f(b, Kpages, Vpages, Kscale, Vscale, K, V, row_stride, head_stride, st); };
-    if (dtype == 0)
-        return form == kPagesPlain ? go(read_rows<float, kPagesPlain>)
-             : form == kPagesFp8   ? go(read_rows<float, kPagesFp8>) : go(read_rows<float, kPagesInt8>);
-    return form == kPagesPlain ? go(read_rows<uint16_t, kPagesPlain>)
-         : form == kPagesFp8   ? go(read_rows<uint16_t, kPagesFp8>) : go(read_rows<uint16_t, kPagesInt8>);
+    return with_form(form, [&](auto f) {
+        constexpr int FORM = decltype(f)::value;
+        auto go = [&](auto read) { return read(b, Kpages, Vpages, Kscale, Vscale, K, V, row_stride, head_stride, st); };
+        return dtype == 0 ? go(read_rows<float, FORM>) : go(read_rows<uint16_t, FORM>);
+    });
 }
 
 }  // namespace gkv

@@ -237,6 +237,9 @@ struct PagedBatch;   // paged.hpp
 // Rows of K and V ([row, head], strides in elements) to the places of their tokens, and back.
 hipError_t launch_cache_write(const PagedBatch &b, int dtype, int form, const void *K, const void *V, long row_stride,
                               long head_stride, void *Kpages, void *Vpages, float *Kscale, float *Vscale, hipStream_t st);
+// (pages in blocks: blocks.hip, by way of the call above)
+hipError_t launch_blocks_write(const PagedBatch &b, int dtype, int form, const void *K, const void *V, long row_stride,
+                               long head_stride, void *Kpages, void *Vpages, float *Kscale, float *Vscale, hipStream_t st);
 hipError_t launch_cache_read(const PagedBatch &b, int dtype, int form, const void *Kpages, const void *Vpages,
                              const float *Kscale, const float *Vscale, void *K, void *V, long row_stride, long head_stride,
                              hipStream_t st);
