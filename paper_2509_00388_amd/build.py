@@ -11,7 +11,8 @@ LIB = os.path.join(HERE, "libgraphkv.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["api.hip", "select.hip", "generic.hip", "gemm.hip", "stages.hip", "mfma_score.hip", "mfma_cosine.hip",
-           "cache.hip", "blocks.hip", "assign.hip", "attend.hip", "attend_few.hip", "attend_many.hip", "attend_wide.hip"]
+           "cache.hip", "blocks.hip", "assign.hip", "attend.hip", "attend_few.hip", "attend_many.hip", "attend_wide.hip",
+           "blocks_attend.hip", "cross_few.hip", "cross_many.hip", "cross_wide.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", 
@@ -35,7 +36,7 @@ def _compile(src: str) -> str:
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
     srcs = [s for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, srcs))
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

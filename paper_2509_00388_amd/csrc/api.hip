@@ -438,20 +438,20 @@ int32_t run_attend(const graphkv_paged_params *p, bool cross, const void *Q, con
     a.G = A.G;
     a.c = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
     hipStream_t st = (hipStream_t)stream;
-    if (A.generic || cross || in_blocks(p->page_format)) {
+    if (A.generic) {
         GKV_LAUNCH(GRAPHKV_K_ATTEND_GENERIC, launch_attend_generic(a, p->dtype, p->page_format, cross, st));
         return GRAPHKV_OK;
     }
     if (A.few) {
         A.fp.join.records = at<JoinRecord>(ws, 0);
         A.fp.join.slots = at<float>(ws, A.few_slots);
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_FEW, launch_attend_few(a, A.fp, p->dtype, p->page_format, cross, st));
     }
     if (A.many) {
         A.mp.join.records = at<JoinRecord>(ws, A.many_records);
         A.mp.join.slots = at<float>(ws, A.many_slots);
-        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, st)
-                                                    : launch_attend_many(a, A.mp, p->dtype, p->page_format, st));
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, cross, st)
+                                                    : launch_attend_many(a, A.mp, p->dtype, p->page_format, cross, st));
     }
     GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, A.mp.join, p->dtype, st));
     return GRAPHKV_OK;

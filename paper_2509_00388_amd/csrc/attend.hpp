@@ -1,4 +1,4 @@
-// Arguments of the attention kernels (attend.hip, attend_few.hip, attend_many.hip).
+// Arguments of the attention kernels (attend.hip, attend_few.hpp, attend_many.hpp, attend_wide.hpp).
 #pragma once
 #include "paged.hpp"
 
@@ -116,7 +116,7 @@ struct ManyPlan {
     JoinPlan join;
     int block_rows, tile_keys, step;
     int leave_few;    // sequences of few rows are the other kernel's
-    int wide;         // blocks of 256 rows (attend_wide.hip)
+    int wide;         // blocks of 256 rows (attend_wide.hpp)
 };
 struct ManySeq {
     int rows, blocks;        // stacked
@@ -124,21 +124,24 @@ struct ManySeq {
     uint32_t per_head;
 };
 // Units of block k of a sequence; `whole`: as if it were full of rows.  (Stacked rows and positions are below 2^31 together.)
+// CROSS: rows are no tokens of the sequence, and all of them see all of it.
+template <bool CROSS>
 __device__ __forceinline__ uint32_t many_units(const SeqRows &q, int rows, int k, bool whole, const AttendArgs &a, const ManyPlan &p)
 {
     const uint32_t end = (uint32_t)(k + 1) * p.block_rows;
-    const int sees = q.len - q.n + (int)(((whole ? end : min(end, (uint32_t)rows)) - 1) / (uint32_t)a.G) + 1;
+    const int sees = CROSS ? q.len : q.len - q.n + (int)(((whole ? end : min(end, (uint32_t)rows)) - 1) / (uint32_t)a.G) + 1;
     const uint32_t keys = (uint32_t)p.tile_keys * p.step;
     return sees <= (int)keys ? 1u : ((uint32_t)sees + keys - 1) / keys;
 }
+template <bool CROSS>
 __device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &a, const ManyPlan &p)
 {
     ManySeq m{};
     if (q.n <= 0 || (p.leave_few && has_few(q, a.G))) return m;
     m.rows = q.n * a.G;
     m.blocks = (m.rows + p.block_rows - 1) / p.block_rows;
-    if (m.blocks > 1) m.pair = many_units(q, m.rows, 0, true, a, p) + many_units(q, m.rows, m.blocks - 1, true, a, p) + 2;
-    if (m.blocks & 1) m.middle = many_units(q, m.rows, m.blocks / 2, false, a, p);
+    if (m.blocks > 1) m.pair = many_units<CROSS>(q, m.rows, 0, true, a, p) + many_units<CROSS>(q, m.rows, m.blocks - 1, true, a, p) + (CROSS ? 0 : 2);
+    if (m.blocks & 1) m.middle = many_units<CROSS>(q, m.rows, m.blocks / 2, false, a, p);
     m.per_head = m.blocks / 2 * m.pair + m.middle;
     return m;
 }
@@ -148,12 +151,13 @@ struct ManyPart {
     int rows, h, block;   // rows: stacked rows of the sequence
     uint32_t u0, u1, units;
 };
+template <bool CROSS>
 __device__ __forceinline__ bool next_part(const AttendArgs &a, const ManyPlan &pl, uint32_t &pos, uint32_t last, int &s,
                                           uint32_t &before, ManyPart &p)
 {
     while (pos < last && s < a.b.n_seqs) {
         p.sq = seq_rows(a.b, s);
-        const ManySeq ms = many_seq(p.sq, a, pl);
+        const ManySeq ms = many_seq<CROSS>(p.sq, a, pl);
         if (ms.per_head == 0 || pos >= before + ms.per_head * a.b.H) {   // the next sequence
             before += ms.per_head * a.b.H;
             ++s;
@@ -166,11 +170,11 @@ __device__ __forceinline__ bool next_part(const AttendArgs &a, const ManyPlan &p
         at -= (uint32_t)pair * ms.pair;
         p.u0 = at;
         p.block = ms.blocks - 1 - pair;
-        p.units = many_units(p.sq, p.rows, p.block, false, a, pl);
+        p.units = many_units<CROSS>(p.sq, p.rows, p.block, false, a, pl);
         if (p.u0 >= p.units) {
             p.u0 -= p.units;
             p.block = pair;
-            p.units = many_units(p.sq, p.rows, pair, false, a, pl);
+            p.units = many_units<CROSS>(p.sq, p.rows, pair, false, a, pl);
             if (p.u0 >= p.units) {   // the pair's empty rest
                 pos += ms.pair - at;
                 continue;
@@ -187,9 +191,16 @@ bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
 ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);   // no workgroups: more units than 31 bits count
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, bool cross, hipStream_t st);
-hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
-hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
-hipError_t launch_attend_wide(const AttendArgs &a, const ManyPlan &pl, int form, hipStream_t st);
+// (`cross`: rows see all of their sequence.  The kernels of each kind are compiled in files of their own: these, blocks_attend.hip, cross_*.hip.)
+hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, bool cross, hipStream_t st);
+hipError_t launch_attend_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, bool cross, hipStream_t st);
+hipError_t launch_attend_wide(const AttendArgs &a, const ManyPlan &pl, int form, bool cross, hipStream_t st);
+hipError_t launch_blocks_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_blocks_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_blocks_wide(const AttendArgs &a, const ManyPlan &pl, int form, hipStream_t st);
+hipError_t launch_cross_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_cross_many(const AttendArgs &a, const ManyPlan &pl, int dtype, int form, hipStream_t st);
+hipError_t launch_cross_wide(const AttendArgs &a, const ManyPlan &pl, int form, hipStream_t st);
 hipError_t launch_attend_join(const AttendArgs &a, const JoinPlan &few, const JoinPlan &many, int dtype, hipStream_t st);   // n_wg 0: none
 inline size_t join_record_bytes(const JoinPlan &p) { return (size_t)p.n_wg * sizeof(JoinRecord); }
 inline size_t join_slot_bytes(const JoinPlan &p) { return (size_t)2 * p.n_wg * p.slot_floats * 4; }

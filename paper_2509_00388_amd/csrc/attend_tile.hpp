@@ -60,8 +60,8 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
     __device__ static __forceinline__ bool odd(const uint4 &v)
     {
         auto any = [&](auto f) { return f(v.x) || f(v.y) || f(v.z) || f(v.w); };
-        if constexpr (FORM == kPagesFp8) return any([](uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; });
-        if constexpr (FORM == kPagesInt8) return false;
+        if constexpr (code_of(FORM) == kPagesFp8) return any([](uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; });
+        if constexpr (code_of(FORM) == kPagesInt8) return false;
         if constexpr (sizeof(T) == 4) return any([](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; });
         return any([](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u; });
     }
@@ -111,7 +111,7 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
         if constexpr (FORM == kPagesPlain) {
             w[0] = v;
         } else {
-            if constexpr (FORM == kPagesFp8 && sizeof(T) == 2) {   // (two codes an instruction, the scale 1)
+            if constexpr (code_of(FORM) == kPagesFp8 && sizeof(T) == 2) {   // (two codes an instruction, the scale 1)
                 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
                 const uint32_t c[4] = {v.x, v.y, v.z, v.w};
                 union { bf16x2 b[8]; uint4 u[2]; } y;
@@ -240,6 +240,25 @@ __device__ __forceinline__ uint64_t seen_keys(uint64_t vis, int limit, int hh)
 // attend_wide, 2048 rows of 32768 keys 1062 / 1032; attend_few, 64 sequences in fp8 98.2 / 97.1.)
 constexpr float kMaxLag = 8.f;
 
+// The reference m brought to the tile's maximum `top` (of all keys so far) where it has to be, sums with it; returns what to take from logits.
+template <int DB>
+__device__ __forceinline__ float follow_maximum(float top, float &m, float &l, f32x16 (&o)[DB])
+{
+    // (The vote only says whether any row has something to do: each row's reference follows its own maxima, so that how its weights are rounded
+    // does not depend on what other rows see.)
+    if (__any(top > m + kMaxLag)) {
+        const bool grown = top > m + kMaxLag;
+        const float fade = grown ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+        l *= fade;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] *= fade;
+        m = grown ? top : m;
+    }
+    return m == -INFINITY ? 0.f : m;   // (nothing seen yet: all weights are 2^-inf)
+}
+
 // One tile of logits (NB blocks of 32 keys) to weights 2^(x - m), with the running reference m (the maximum, or up to kMaxLag below it) and
 // sum l of the lane's query; o is brought to the new one.  ks: the keys' scales times c (8-bit), NB x 32 of them; c: otherwise.
 // `all`: every row sees every key; otherwise `seen` has the keys that the lane's query sees (seen_keys()).
@@ -268,20 +287,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
-    top = fmaxf(m, other_half_max(top) * c);   // (c > 0)
-    // (The vote only says whether any row has something to do: each row's reference follows its own maxima, so that how its weights are rounded
-    // does not depend on what other rows see.)
-    if (__any(top > m + kMaxLag)) {
-        const bool grown = top > m + kMaxLag;
-        const float fade = grown ? __builtin_amdgcn_exp2f(m - top) : 1.f;
-        l *= fade;
-#pragma unroll
-        for (int b = 0; b < DB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[b][i] *= fade;
-        m = grown ? top : m;
-    }
-    const float shift = m == -INFINITY ? 0.f : m;   // (nothing seen yet: all weights are 2^-inf)
+    const float shift = follow_maximum<DB>(fmaxf(m, other_half_max(top) * c), m, l, o);   // (c > 0)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -290,6 +296,61 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
             l += p[b][i];
         }
 }
+
+// The same where 16 keys from a multiple of 16 on share a scale (pages in blocks): kc[g]: the scale of group g's keys times c, vs[g], log_vs[g], inv_vs[g]: that of
+// its values, its logarithm to base 2 and its inverse, all above 0.  The weights come out times the values' scales.  With bf16 rows that costs nothing: the scale's
+// logarithm goes into the exponent, and the sum takes a group's weights back to their own size; the exponent is rounded once more, by some
+// 2^-20, far below the weights' own rounding to bf16.  With fp32 rows they are multiplied.
+template <bool FOLD, int NB, int DB>
+__device__ __forceinline__ void softmax_blocks(f32x16 (&x)[NB], const float (&kc)[2 * NB], const float (&vs)[2 * NB], const float (&log_vs)[2 * NB],
+                                               const float (&inv_vs)[2 * NB], bool all, uint64_t seen, int hh, float &m, float &l,
+                                               f32x16 (&o)[DB], float (&p)[NB][16])
+{
+    if (!all) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[b][i] = (seen >> (32 * b + acc_row(i, 0))) & 1 ? x[b][i] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+        float most = x[g / 2][8 * (g & 1)];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) most = fmaxf(most, x[g / 2][8 * (g & 1) + i]);
+        top = fmaxf(top, most * kc[g]);
+    }
+    const float shift = follow_maximum<DB>(fmaxf(m, other_half_max(top)), m, l, o);
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+        const float from = FOLD ? log_vs[g] - shift : -shift;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float &w = p[g / 2][8 * (g & 1) + i];
+            w = __builtin_amdgcn_exp2f(fmaf(x[g / 2][8 * (g & 1) + i], kc[g], from));
+            sum += w;
+            if (!FOLD) w *= vs[g];
+        }
+        l = FOLD ? fmaf(sum, inv_vs[g], l) : l + sum;
+    }
+}
+// The same with the groups' numbers from the LDS: kc at ks[0], log_vs (fp32 rows: vs) at ks[4] and inv_vs at ks[8] on.
+template <typename T, int NB, int DB>
+__device__ __forceinline__ void softmax_groups(f32x16 (&x)[NB], const float *ks, bool all, uint64_t seen, int hh, float &m, float &l,
+                                               f32x16 (&o)[DB], float (&p)[NB][16])
+{
+    float kc[2 * NB], vs[2 * NB], inv_vs[2 * NB];
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+        kc[g] = ks[g];
+        vs[g] = ks[4 + g];
+        inv_vs[g] = ks[8 + g];
+    }
+    softmax_blocks<sizeof(T) == 2, NB, DB>(x, kc, vs, vs, inv_vs, all, seen, hh, m, l, o, p);
+}
+// A scale as those need it: 0, which a block of zeros has, counts as 1.
+__device__ __forceinline__ float above_zero(float scale) { return scale > 0.f ? scale : 1.f; }
 
 // The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
 template <int NB>
@@ -354,7 +415,7 @@ __device__ __forceinline__ void add_odd_rows(const AttendArgs &a, int s, int h, 
         x = other_half_sum(x) * a.c;
         float w;
         if constexpr (FORM == kPagesPlain) w = __builtin_amdgcn_exp2f(x - m);
-        else w = __builtin_amdgcn_exp2f(x * a.Kscale[row] - m) * a.Vscale[row];
+        else w = __builtin_amdgcn_exp2f(x * a.Kscale[scale_of_row<FORM>(a.b, (int)row)] - m) * a.Vscale[scale_of_row<FORM>(a.b, (int)row)];
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll

@@ -178,12 +178,13 @@ def test_many_sequences(dtype):
     pu.check_attend(b, Q, out, lse)
 
 
+@pytest.mark.parametrize("impl", IMPLS)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("form", FORMS)
-def test_a_row_over_its_own_tokens(dtype, form):
+def test_a_row_over_its_own_tokens(dtype, form, impl):
     """A sequence's last row sees the same positions as in causal attention: the same bits where each sequence has one row."""
     say(f"cross and causal dtype={dtype} form={form}")
-    b = mu.Batch([(1, 300), (1, 1), (1, 64), (1, 1000)], H=2, G=4, d=128, ps=64, dtype=dtype, form=form, impl=gk.IMPL_GENERIC)
+    b = mu.Batch([(1, 300), (1, 1), (1, 64), (1, 1000)], H=2, G=4, d=128, ps=64, dtype=dtype, form=form, impl=impl)
     Q, args = on_gpu(b.random_rows(8)), b.device()
     lse = [torch.empty(4, 8, device="cuda") for _ in range(2)]
     want = gk.graphkv_attend(b.p, Q, *args, lse=lse[0])
