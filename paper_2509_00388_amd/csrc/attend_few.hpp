@@ -21,7 +21,8 @@ namespace {
 
 // A wave's place in the LDS: KEYS rows of keys, then of values, and the scales of both.
 template <typename T, int FORM, int D, int NB> struct WavePlace {
-    static constexpr int kPitch = Tile<T, FORM, D, 32 * NB, 64>::kKeyPitch, kRows = 32 * NB * kPitch;
+    using L = Tile<T, FORM, D, 32 * NB, 64>;
+    static constexpr int kPitch = L::kKeyPitch, kValues = L::kHalves ? L::kValPitch : kPitch, kRows = 32 * NB * kValues;   // kValues >= kPitch
     static constexpr int kBytes = kRows + (FORM == kPagesPlain || in_blocks(FORM) ? 0 : 2 * 32 * NB * 4);
 };
 

@@ -50,8 +50,25 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
     static constexpr int kPer = (KEYS * kPieces + NT - 1) / NT;                  // pieces of a thread
     static constexpr bool kSpare = KEYS * kPieces < NT;                          // threads without one
     static constexpr int kRowStep = NT / kPieces;                                // rows between two of its pieces
-    static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 32);
+    // Sixteen codes are 32 bytes in the LDS: two writes of 16.  In one place they would lie 32 bytes from those of the next lane, and half of the
+    // banks would take them all; so the first halves of a segment's eight pieces lie together, the second halves 128 bytes behind.  (us, so / in one
+    // place, pages in blocks: 2000 rows of four query heads a key head over 24000 keys, fp8 775 / 842, int8 758 / 818; six sequences of 445 rows over 1000 to 9000 states 175 / 190;
+    // 64 tokens over 400 to 5000 keys the same.  Not with a scale a row, where the largest fp8 variant has no registers for it: 949 / 931.)
+    static constexpr bool kHalves = in_blocks(FORM) && sizeof(T) == 2 && D >= 128;
+    static constexpr int kKeyPitch = D * (int)sizeof(T) + 16, kValPitch = D * (int)sizeof(T) + (sizeof(T) == 2 && !kHalves ? 64 : 32);
     static constexpr int kDecoded = 16 / kCached * (int)sizeof(T);               // bytes of a piece in the LDS
+    static constexpr int kHalf = kHalves ? 128 : 16;                             // between the two of a piece
+    // Where a piece lies in a row.
+    __device__ static __forceinline__ constexpr int piece_at(int piece) { return kHalves ? (piece >> 3) * 256 + (piece & 7) * 16 : piece * kDecoded; }
+    // The 32 bytes of a row of keys that a matrix step takes: 16 of them here, 16 kHalf further.
+    __device__ static __forceinline__ constexpr int step_at(int step) { return kHalves ? (step >> 3) * 256 + (step & 7) * 16 : 32 * step; }
+    // Where a lane's values for the transposing reads of a block of 32 dimensions lie in a row.
+    __device__ static __forceinline__ int value_at(int lane)
+    {
+        const int i = lane & 3, group = (lane >> 4) & 1;
+        return kHalves ? group * 16 + (i >> 1) * 128 + (i & 1) * 8 : group * 32 + i * 8;
+    }
+    __device__ static __forceinline__ constexpr int block_at(int block) { return kHalves ? (block >> 2) * 256 + (block & 3) * 32 : 64 * block; }
     static constexpr int kSteps = D * (int)sizeof(T) / 32;                       // matrix steps of a row of keys
     static constexpr int kWaveRows = 64 / kPieces < 1 ? 1 : 64 / kPieces;        // rows of a wave's turn, next to one another
     static_assert((kSpare || KEYS * kPieces % NT == 0) && NT % kPieces == 0, "whole rows a turn");
@@ -121,7 +138,7 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
                     y.b[2 * e + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.f, true);
                 }
                 w[0] = y.u[0];
-                w[1] = y.u[1];
+                w[kHalf / 16] = y.u[1];
                 return;
             }
             float x[16];
@@ -133,7 +150,7 @@ template <typename T, int FORM, int D, int KEYS, int NT> struct Tile {
             } else {   // (codes are exact in bf16)
 #pragma unroll
                 for (int e = 0; e < 16; e += 8)
-                    w[e / 8] = make_uint4(pack_bf16(x[e], x[e + 1]), pack_bf16(x[e + 2], x[e + 3]),
+                    w[e / 8 * (kHalf / 16)] = make_uint4(pack_bf16(x[e], x[e + 1]), pack_bf16(x[e + 2], x[e + 3]),
                                           pack_bf16(x[e + 4], x[e + 5]), pack_bf16(x[e + 6], x[e + 7]));
             }
         }
@@ -176,31 +193,31 @@ __device__ __forceinline__ Weights pack_weights(const float (&p)[16])
     return r;
 }
 
-// O^T += V^T P^T over a block of 32 keys: vt is the block's first row of values in the LDS.
-template <int D, int PITCH>
+// O^T += V^T P^T over a block of 32 keys: vt is the block's first row of values in the LDS, as L lays it out with PITCH bytes a row.
+template <typename L, int D, int PITCH>
 __device__ __forceinline__ void add_values(const unsigned char *vt, const Weights &p, int lane, f32x16 (&o)[D / 32])
 {
     const int i = lane & 15, hh = lane >> 5;
-    const unsigned char *at = vt + (4 * hh + (i >> 2)) * PITCH + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+    const unsigned char *at = vt + (4 * hh + (i >> 2)) * PITCH + L::value_at(lane);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int b = 0; b < D / 32; ++b) {
             // two groups of four keys, as acc_row() deals them out
             typedef __attribute__((address_space(3))) bf16x4 lds4;
-            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + 16 * s * PITCH + 64 * b));
-            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + (16 * s + 8) * PITCH + 64 * b));
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + 16 * s * PITCH + L::block_at(b)));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + (16 * s + 8) * PITCH + L::block_at(b)));
             o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p.w[s], o[b], 0, 0, 0);
         }
 }
-template <int D, int PITCH>
+template <typename L, int D, int PITCH>
 __device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], uint16_t)
 {
-    add_values<D, PITCH>(vt, pack_weights(p), lane, o);
+    add_values<L, D, PITCH>(vt, pack_weights(p), lane, o);
 }
 // The same with weights in two bf16 operands: the first cut off, the second what that leaves, at most 2^-7 of the weight and rounded by 2^-8 of
 // itself.  Where an infinite value meets them, both have to be above 0 (inf - inf, 0 x inf): the second is 2^-22 of the weight too large.
-template <int D, int PITCH>
+template <typename L, int D, int PITCH>
 __device__ __forceinline__ void add_values_twice(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32])
 {
     float high[16], rest[16];
@@ -209,10 +226,10 @@ __device__ __forceinline__ void add_values_twice(const unsigned char *vt, const 
         high[i] = __uint_as_float(__float_as_uint(p[i]) & 0xffff0000u);
         rest[i] = fmaf(p[i], 1.f + 0x1p-22f, -high[i]);
     }
-    add_values<D, PITCH>(vt, pack_weights(high), lane, o);
-    add_values<D, PITCH>(vt, pack_weights(rest), lane, o);
+    add_values<L, D, PITCH>(vt, pack_weights(high), lane, o);
+    add_values<L, D, PITCH>(vt, pack_weights(rest), lane, o);
 }
-template <int D, int PITCH>
+template <typename L, int D, int PITCH>
 __device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], float)
 {
     const unsigned char *at = vt + 4 * (lane >> 5) * PITCH + (lane & 31) * 4;
