@@ -76,6 +76,9 @@ __device__ __forceinline__ int stretch_owner(uint32_t total, uint32_t unit, int 
     return min((int)((((uint64_t)unit + 1) * n - 1) / total), n - 1);
 }
 
+// stretch_first() with 32 bits, for few workgroups: total = q n + r, so that total w / n = q w + r w / n.
+__device__ __forceinline__ uint32_t few_first(uint32_t total, uint32_t w, uint32_t n) { return total / n * w + total % n * w / n; }
+
 // What a workgroup leaves of a block of rows that others hold parts of too: every workgroup has two slots, for the part its
 // stretch begins with and the part it ends with, and a record of a block whose first part it holds.  The other parts of
 // that block are the first slots of the workgroups behind it.
