@@ -4,8 +4,8 @@
 // a block which holds earlier tokens keep its scale if it is enough for them; otherwise the scale grows to theirs, and the codes that are there are
 // rounded again, round(code * old / new): a power of two apart for e4m3, in 64 bits for integers.
 //
-// A workgroup takes a block of a head: the largest magnitude of its new rows, then their codes; rows stay in registers between the two where they
-// are few enough, else they are read again.  Blocks are found by their first new row: a workgroup looks at a stretch of rows for those that
+// A wave or a workgroup takes a block of a head: the largest magnitude of its new rows, then their codes; rows stay in registers between the two where
+// they are few enough, else they are read again.  Blocks are found by their first new row: a workgroup looks at a stretch of rows for those that
 // begin one.
 #include "kernels.hpp"
 #include "paged.hpp"
@@ -14,7 +14,9 @@ namespace gkv {
 
 namespace {
 
-constexpr int kHeld = 4;   // pieces of each tensor that a thread keeps between its two passes
+
+// The largest of a wave's numbers that are not below 0, in all lanes.
+__device__ __forceinline__ float wave_largest(float x) { return __uint_as_float(wave_max_u32(__float_as_uint(x))); }
 
 // Codes 0 .. 15 of a piece, to the scale `after`.
 template <int FORM> __device__ __forceinline__ uint4 encode_again(const uint4 &v, float before, float after)
@@ -65,87 +67,109 @@ struct BlocksWrite {
     int group, stretch;   // lanes of a row, rows that a workgroup looks at
 };
 
-template <typename T, int FORM>
+// A block of a head is WAVES waves' work: of one, so that four heads share a workgroup, or of all four.  HELD: pieces of each tensor that a thread
+// keeps between the two passes over the block's rows.
+template <typename T, int FORM, int WAVES, int HELD>
 __global__ __launch_bounds__(256) void blocks_write_kernel(PagedBatch b, BlocksWrite w)
 {
-    constexpr int PER = Elem<T>::kPerVec;
+    constexpr int PER = Elem<T>::kPerVec, THREADS = 64 * WAVES;
     __shared__ float tops[2][4];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, h = blockIdx.y;
-    const int at = tid & (w.group - 1), mine = tid / w.group, step = 256 / w.group, pieces = b.d / PER;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = WAVES == 1 ? blockIdx.y * 4 + wv : blockIdx.y, tid = WAVES == 1 ? lane : threadIdx.x;
+    if (h >= b.H) return;
+    const int at = tid & (w.group - 1), mine = tid / w.group, step = THREADS / w.group, pieces = b.d / PER;
     const int tokens = 1 << b.scale_shift;
     const T *K = reinterpret_cast<const T *>(w.K) + h * w.head_stride, *V = reinterpret_cast<const T *>(w.V) + h * w.head_stride;
 
     const int last = min((int)(blockIdx.x + 1) * w.stretch, b.n_rows);
+    SeqRows q{0, 0, 0};
+    int s = -1, turn = blockIdx.z;   // of the blocks that begin in the stretch, every gridDim.z-th from there on is this workgroup's
     for (int row = blockIdx.x * w.stretch; row < last;) {
-        const int s = seq_of_row(b, row, lane);
-        if (s >= b.n_seqs) break;
-        const SeqRows q = seq_rows(b, s);
+        if (s < 0 || row >= q.row0 + q.n) {
+            s = seq_of_row(b, row, lane);
+            if (s >= b.n_seqs) break;
+            q = seq_rows(b, s);
+        }
         const int i = row - q.row0, pos = q.len - q.n + i;
-        if (i < 0 || i >= q.n) { ++row; continue; }
+        if (i < 0 || i >= q.n) { ++row; s = -1; continue; }
         if (pos < 0) { row += min(-pos, q.n - i); continue; }
         const int inside = pos & (tokens - 1);
         const int rest = min(tokens - inside, q.len - pos);   // rows up to the block's end or the sequence's
-        if (inside > 0 && i > 0 && pos > 0) { row += rest; continue; }   // the block's first new row is another's
-        const int first = row, page = page_of(b, s, pos);
+        const int first = row;
         row += rest;
+        if (inside > 0 && i > 0) continue;   // the block's first new row is another's
+        if (turn-- > 0) continue;
+        turn = gridDim.z - 1;
+        const int page = page_of(b, s, pos);
         if (page < 0) continue;
 
         const int base = pool_row(b, page, h, pos - inside), block = base >> b.scale_shift;
-        const bool held = rest <= kHeld * step && pieces <= w.group;
-        uint4 kv[kHeld], vv[kHeld];
-        float ka = 0.f, va = 0.f;
+        const float kb = inside > 0 ? w.Kscale[block] : 0.f, vb = inside > 0 ? w.Vscale[block] : 0.f;
+        char *kto = reinterpret_cast<char *>(w.Kpages) + (long)base * b.d, *vto = reinterpret_cast<char *>(w.Vpages) + (long)base * b.d;
         auto row_of = [&](const T *x, int r) { return reinterpret_cast<const uint4 *>(x + (first + r) * w.row_stride); };
-        if (held) {
+        float ks, vs, kinv, vinv;
+        // The block's scales, from its new rows' largest magnitudes; codes that are there to the new ones.
+        auto settle = [&](float ka, float va) {
+            ka = wave_largest(ka);
+            va = wave_largest(va);
+            if constexpr (WAVES > 1) {
+                __syncthreads();   // (the block before is done with them)
+                if (lane == 0) { tops[0][wv] = ka; tops[1][wv] = va; }
+                __syncthreads();
+                ka = fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3]));
+                va = fmaxf(fmaxf(tops[1][0], tops[1][1]), fmaxf(tops[1][2], tops[1][3]));
+            }
+            ks = fmaxf(kb, scale_of<FORM>(ka));
+            vs = fmaxf(vb, scale_of<FORM>(va));
+            kinv = ks > 0.f ? 1.f / ks : 0.f;
+            vinv = vs > 0.f ? 1.f / vs : 0.f;
+            if (tid == 0) { w.Kscale[block] = ks; w.Vscale[block] = vs; }
+            const int old = kb < ks || vb < vs ? inside * (b.d / 16) : 0;   // (the codes before the first new row are a run of them)
+#pragma unroll 1
+            for (int p = tid; p < old; p += THREADS) {
+                if (kb < ks) { uint4 *x = reinterpret_cast<uint4 *>(kto) + p; *x = encode_again<FORM>(*x, kb, ks); }
+                if (vb < vs) { uint4 *x = reinterpret_cast<uint4 *>(vto) + p; *x = encode_again<FORM>(*x, vb, vs); }
+            }
+            kto += (long)inside * b.d;
+            vto += (long)inside * b.d;
+        };
+        if (rest <= HELD * step && pieces <= w.group) {
+            const int turns = (rest + step - 1) / step;
+            uint4 kv[HELD], vv[HELD];
+            float ka = 0.f, va = 0.f;
 #pragma unroll
-            for (int t = 0; t < kHeld; ++t) {
-                const int r = mine + t * step;
-                const bool in = at < pieces && r < rest;
-                kv[t] = in ? row_of(K, r)[at] : make_uint4(0, 0, 0, 0);
-                vv[t] = in ? row_of(V, r)[at] : make_uint4(0, 0, 0, 0);
+            for (int t = 0; t < HELD; ++t) {   // (a turn or lane without a piece takes another's: neither largest nor code changes by that)
+                const int r = min(mine + min(t, turns - 1) * step, rest - 1), p = min(at, pieces - 1);
+                kv[t] = row_of(K, r)[p];
+                vv[t] = row_of(V, r)[p];
             }
 #pragma unroll
-            for (int t = 0; t < kHeld; ++t) {
+            for (int t = 0; t < HELD; ++t) {
                 ka = largest_of<T>(kv[t], ka);
                 va = largest_of<T>(vv[t], va);
             }
+            settle(ka, va);
+#pragma unroll
+            for (int t = 0; t < HELD; ++t)   // (what was unpacked for the largest is not kept: it would take the registers of half the waves)
+                asm volatile("" : "+v"(kv[t].x), "+v"(kv[t].y), "+v"(kv[t].z), "+v"(kv[t].w), "+v"(vv[t].x), "+v"(vv[t].y), "+v"(vv[t].z), "+v"(vv[t].w));
+#pragma unroll
+            for (int t = 0; t < HELD; ++t)
+                if (t < turns) {
+                    const int to = min(mine + t * step, rest - 1) * b.d + min(at, pieces - 1) * PER;
+                    put_codes<T, FORM>(kto + to, kv[t], ks, kinv);
+                    put_codes<T, FORM>(vto + to, vv[t], vs, vinv);
+                }
         } else {
+            float ka = 0.f, va = 0.f;
             for (int r = mine; r < rest; r += step)
+#pragma unroll 1
                 for (int p = at; p < pieces; p += w.group) {
                     ka = largest_of<T>(row_of(K, r)[p], ka);
                     va = largest_of<T>(row_of(V, r)[p], va);
                 }
-        }
-        const float kb = inside > 0 ? w.Kscale[block] : 0.f, vb = inside > 0 ? w.Vscale[block] : 0.f;
-        ka = wave_max(ka);
-        va = wave_max(va);
-        __syncthreads();   // (the block before is done with them)
-        if (lane == 0) { tops[0][wv] = ka; tops[1][wv] = va; }
-        __syncthreads();
-        ka = fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3]));
-        va = fmaxf(fmaxf(tops[1][0], tops[1][1]), fmaxf(tops[1][2], tops[1][3]));
-        const float ks = fmaxf(kb, scale_of<FORM>(ka)), vs = fmaxf(vb, scale_of<FORM>(va));
-        const float kinv = ks > 0.f ? 1.f / ks : 0.f, vinv = vs > 0.f ? 1.f / vs : 0.f;
-        if (tid == 0) { w.Kscale[block] = ks; w.Vscale[block] = vs; }
-        char *kto = reinterpret_cast<char *>(w.Kpages) + (long)base * b.d, *vto = reinterpret_cast<char *>(w.Vpages) + (long)base * b.d;
-        if (kb < ks || vb < vs) {
-            const int old = inside * (b.d / 16);   // (the codes before the first new row are a run of them)
-            for (int p = tid; p < old; p += 256) {
-                if (kb < ks) { uint4 *x = reinterpret_cast<uint4 *>(kto) + p; *x = encode_again<FORM>(*x, kb, ks); }
-                if (vb < vs) { uint4 *x = reinterpret_cast<uint4 *>(vto) + p; *x = encode_again<FORM>(*x, vb, vs); }
-            }
-        }
-        kto += (long)inside * b.d;
-        vto += (long)inside * b.d;
-        if (held) {
-#pragma unroll
-            for (int t = 0; t < kHeld; ++t) {
-                const int r = mine + t * step;
-                if (at >= pieces || r >= rest) continue;
-                put_codes<T, FORM>(kto + (long)r * b.d + at * PER, kv[t], ks, kinv);
-                put_codes<T, FORM>(vto + (long)r * b.d + at * PER, vv[t], vs, vinv);
-            }
-        } else {
+            settle(ka, va);
             for (int r = mine; r < rest; r += step)
+#pragma unroll 1
                 for (int p = at; p < pieces; p += w.group) {
                     put_codes<T, FORM>(kto + (long)r * b.d + p * PER, row_of(K, r)[p], ks, kinv);
                     put_codes<T, FORM>(vto + (long)r * b.d + p * PER, row_of(V, r)[p], vs, vinv);
@@ -164,13 +188,25 @@ hipError_t launch_blocks_write(const PagedBatch &b, int dtype, int form, const v
     while (group < pieces && group < kWave) group <<= 1;
     // Stretches of a block's tokens, in which a long sequence begins one block; where sequences have fewer rows than that, or the rows are few
     // altogether, a row each.
-    const int tokens = 1 << b.scale_shift;
+    const int tokens = 1 << b.scale_shift, most = b.max_rows < tokens ? b.max_rows : tokens;   // new rows of a block
     const bool single = b.max_rows < tokens || (long)b.n_rows * b.H <= 4096;
     const BlocksWrite w{K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, group, single ? 1 : tokens};
-    const dim3 grid((b.n_rows + w.stretch - 1) / w.stretch, b.H);
+    const int at_once = kWave / group;   // rows that a wave takes at once
+    const bool one_wave = most <= 8 * at_once;
+    // (Two workgroups a stretch where several sequences may begin a block each in it.)
+    const dim3 grid((b.n_rows + w.stretch - 1) / w.stretch, one_wave ? (b.H + 3) / 4 : b.H, !single && b.n_seqs > 1 ? 2 : 1);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(b, w); return hipGetLastError(); };
-    if (dtype == 0) return form == kBlocksFp8 ? go(blocks_write_kernel<float, kBlocksFp8>) : go(blocks_write_kernel<float, kBlocksInt8>);
-    return form == kBlocksFp8 ? go(blocks_write_kernel<uint16_t, kBlocksFp8>) : go(blocks_write_kernel<uint16_t, kBlocksInt8>);
+    auto with_size = [&](auto type, auto f) {
+        using T = decltype(type);
+        constexpr int FORM = decltype(f)::value;
+        return most <= at_once ? go(blocks_write_kernel<T, FORM, 1, 1>)
+             : one_wave        ? go(blocks_write_kernel<T, FORM, 1, 8>) : go(blocks_write_kernel<T, FORM, 4, 4>);
+    };
+    auto with_type = [&](auto f) {
+        if (dtype == 0) return with_size(float{}, f);
+        return with_size(uint16_t{}, f);
+    };
+    return form == kBlocksFp8 ? with_type(std::integral_constant<int, kBlocksFp8>{}) : with_type(std::integral_constant<int, kBlocksInt8>{});
 }
 
 }  // namespace gkv
