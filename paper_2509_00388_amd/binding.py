@@ -137,12 +137,8 @@ class PagedParams:
         return torch.float8_e4m3fn if f in (PAGES_FP8, PAGES_FP8_BLOCKS) else torch.int8 if f in (PAGES_INT8, PAGES_INT8_BLOCKS) else self.torch_dtype
 
     @property
-    def in_blocks(self) -> bool:
-        return self.page_format in (PAGES_FP8_BLOCKS, PAGES_INT8_BLOCKS)
-
-    @property
     def tokens_a_scale(self) -> int:
-        return (self.scale_tokens or min(32, self.page_tokens)) if self.in_blocks else 1
+        return (self.scale_tokens or min(32, self.page_tokens)) if self.page_format >= PAGES_FP8_BLOCKS else 1
 
 
 _lib = None
@@ -424,20 +420,20 @@ def graphkv_compress_batched(p: Params, n_layers: int, budgets, Kc, Vc, Qw, Kout
 # ---- paged cache ----
 # (These calls sit between the kernels of a decoding step, a few microseconds each, so their checks are kept short.)
 
-def _paged_arg(t, name: str, dtype, numel: int, dev):
-    """_arg() for a tensor on a device that is known already."""
-    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and t.is_contiguous() and t.numel() >= numel:
+def _paged_arg(t, name: str, dtype, numel: int, dev: int, _Tensor=torch.Tensor):
+    """_arg() for a tensor on a device (its index) that is known already."""
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= numel:
         return t.data_ptr()
     _arg(t, name, dtype, numel)
-    raise GraphKVError(f"{name} must be on {dev}, where the pools are")
+    raise GraphKVError(f"{name} must be on cuda:{dev}, where the pools are")
 
 
 def _rows_arg(p: PagedParams, t, name: str, heads: int, dev):
     """(address, strides) of a tensor [n_rows, heads, d], any strides that keep a row's d values together."""
     d = p.head_dim
-    if not isinstance(t, torch.Tensor) or t.device != dev:
-        raise GraphKVError(f"{name} must be a tensor on {dev}, where the pools are")
-    if t.dtype != p.torch_dtype:
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        raise GraphKVError(f"{name} must be a tensor on cuda:{dev}, where the pools are")
+    if t.dtype is not p.torch_dtype:
         raise GraphKVError(f"{name} must have dtype {p.torch_dtype}, got {t.dtype}")
     if t.shape != (p.n_rows, heads, d):
         raise GraphKVError(f"{name} must have shape {(p.n_rows, heads, d)}, got {tuple(t.shape)}")
@@ -456,10 +452,10 @@ def _rows_arg(p: PagedParams, t, name: str, heads: int, dev):
 
 
 def _pool_args(p: PagedParams, Kpages, Vpages, table, seq_len, row_start, Kscale, Vscale):
-    """Addresses of what the calls on a paged cache share, checked; the device they live on."""
+    """Addresses of what the calls on a paged cache share, checked; the index of the device they live on."""
     if not isinstance(Kpages, torch.Tensor) or not Kpages.is_cuda:
         raise GraphKVError("Kpages must be a contiguous device tensor")
-    dev, rows, dtype = Kpages.device, p.n_pages * p.n_kv_heads * p.page_tokens, p.page_dtype
+    dev, rows, dtype = Kpages.get_device(), p.n_pages * p.n_kv_heads * p.page_tokens, p.page_dtype
     ks = vs = None
     if p.page_format != PAGES_PLAIN:
         scales = rows // p.tokens_a_scale
@@ -472,19 +468,19 @@ def _pool_args(p: PagedParams, Kpages, Vpages, table, seq_len, row_start, Kscale
 
 
 def _new_rows(p: PagedParams, heads: int, dev):
-    return torch.empty((p.n_rows, heads, p.head_dim), dtype=p.torch_dtype, device=dev)
+    return torch.empty((p.n_rows, heads, p.head_dim), dtype=p.torch_dtype, device=dev)   # (dev: an index)
 
 
 # (torch.cuda.current_stream() builds an object for it: 2.8 us where this takes 0.1)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _call_on(dev, f, *args):
+def _call_on(dev: int, f, *args):
     """Calls f(*args, stream) with the tensors' device as the current one, on that device's current stream."""
-    if dev.index == torch.cuda.current_device():
-        return f(*args, _raw_stream(dev.index))
+    if dev == torch._C._cuda_getDevice():
+        return f(*args, _raw_stream(dev))
     with torch.cuda.device(dev):
-        return f(*args, _raw_stream(dev.index))
+        return f(*args, _raw_stream(dev))
 
 
 def graphkv_cache_write(p: PagedParams, K, V, Kpages, Vpages, table, seq_len, row_start, Kscale=None, Vscale=None):
@@ -565,24 +561,22 @@ def graphkv_cache_assign(p: PagedParams, new_rows, len_before, table, free_pages
     position and the place in the pool of each row."""
     if not isinstance(table, torch.Tensor) or not table.is_cuda:
         raise GraphKVError("table must be a contiguous device tensor")
-    dev, n, lib = table.device, p.n_seqs, load_library()
+    dev, n, lib = table.get_device(), p.n_seqs, load_library()
 
     def new(t, count):
         return torch.empty(count, dtype=torch.int32, device=dev) if t is None else t
     seq_len, free_after, row_start = new(seq_len, n), new(free_after, 1), new(row_start, n + 1)
 
-    def arg(t, name, count):
-        return _paged_arg(t, name, torch.int32, count, dev)
-    cp = p.c()
+    i32, arg, cp = torch.int32, _paged_arg, p.c()
     if ws is None and n > 1024:   # (fewer sequences use none)
         ws = torch.empty(lib.graphkv_assign_workspace_bytes(ctypes.byref(cp)), dtype=torch.uint8, device=dev)
-    wp, wn = (None, 0) if ws is None else (_paged_arg(ws, "ws", torch.uint8, 0, dev), ws.numel())
-    _check(_call_on(dev, lib.graphkv_cache_assign, ctypes.byref(cp), None if keep is None else arg(keep, "keep", n),
-                    arg(new_rows, "new_rows", n), arg(len_before, "len_before", n), arg(seq_len, "seq_len", n),
-                    arg(table, "table", n * p.table_pages), arg(free_pages, "free_pages", p.n_pages), arg(free_before, "free_before", 1),
-                    arg(free_after, "free_after", 1), arg(row_start, "row_start", n + 1),
-                    None if positions is None else arg(positions, "positions", p.n_rows),
-                    None if slots is None else arg(slots, "slots", p.n_rows), wp, wn))
+    wp, wn = (None, 0) if ws is None else (arg(ws, "ws", torch.uint8, 0, dev), ws.numel())
+    _check(_call_on(dev, lib.graphkv_cache_assign, ctypes.byref(cp), None if keep is None else arg(keep, "keep", i32, n, dev),
+                    arg(new_rows, "new_rows", i32, n, dev), arg(len_before, "len_before", i32, n, dev), arg(seq_len, "seq_len", i32, n, dev),
+                    arg(table, "table", i32, n * p.table_pages, dev), arg(free_pages, "free_pages", i32, p.n_pages, dev),
+                    arg(free_before, "free_before", i32, 1, dev), arg(free_after, "free_after", i32, 1, dev),
+                    arg(row_start, "row_start", i32, n + 1, dev), None if positions is None else arg(positions, "positions", i32, p.n_rows, dev),
+                    None if slots is None else arg(slots, "slots", i32, p.n_rows, dev), wp, wn))
     return seq_len, free_after, row_start
 
 

@@ -46,6 +46,17 @@ template <int NW, typename W, typename F>
 __device__ int find_share(int n_seqs, uint32_t &total, uint32_t &before, uint32_t *part, W &&weight, F &&first)
 {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    if (n_seqs <= kWave) {   // (each wave finds it for itself: nothing to wait for)
+        const uint32_t w = lane < n_seqs ? weight(lane) : 0, sums = wave_scan_add(w);
+        total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kWave - 1);
+        const int64_t unit = first(total);
+        if (unit < 0) return -1;
+        const uint64_t behind = __ballot((int64_t)sums > unit);
+        if (behind == 0) return n_seqs;
+        const int s = __ffsll((unsigned long long)behind) - 1;
+        before = (uint32_t)__builtin_amdgcn_readlane((int)(sums - w), s);
+        return s;
+    }
     uint32_t w = tid < n_seqs ? weight(tid) : 0;
     if (tid == 0) part[16] = (uint32_t)n_seqs;   // (found nowhere: only where row numbers that do not ascend overflow the sums)
     uint32_t at = block_scan_add<NW>(w, part, lane, wv, total);
