@@ -319,8 +319,8 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&x)[NB], const float *ks, f
 // logarithm goes into the exponent, and the sum takes a group's weights back to their own size; the exponent is rounded once more, by some
 // 2^-20, far below the weights' own rounding to bf16.  With fp32 rows they are multiplied.
 template <bool FOLD, int NB, int DB>
-__device__ __forceinline__ void softmax_blocks(f32x16 (&x)[NB], const float (&kc)[2 * NB], const float (&vs)[2 * NB], const float (&log_vs)[2 * NB],
-                                               const float (&inv_vs)[2 * NB], bool all, uint64_t seen, int hh, float &m, float &l,
+__device__ __forceinline__ void softmax_blocks(f32x16 (&x)[NB], float (&kc)[2 * NB], float (&vs)[2 * NB], float (&log_vs)[2 * NB],
+                                               float (&inv_vs)[2 * NB], bool all, uint64_t seen, int hh, float &m, float &l,
                                                f32x16 (&o)[DB], float (&p)[NB][16])
 {
     if (!all) {
@@ -328,6 +328,15 @@ __device__ __forceinline__ void softmax_blocks(f32x16 (&x)[NB], const float (&kc
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[b][i] = (seen >> (32 * b + acc_row(i, 0))) & 1 ? x[b][i] : -INFINITY;
+        // (the scales of a group that the lane sees nothing of may be anything)
+#pragma unroll
+        for (int g = 0; g < 2 * NB; ++g) {
+            const bool any = ((seen >> (32 * (g / 2) + 16 * (g & 1))) & 0x0f0f) != 0;
+            kc[g] = any ? kc[g] : 1.f;
+            vs[g] = any ? vs[g] : 1.f;
+            log_vs[g] = any ? log_vs[g] : 0.f;
+            inv_vs[g] = any ? inv_vs[g] : 1.f;
+        }
     }
     float top = -INFINITY;
 #pragma unroll
@@ -357,17 +366,17 @@ template <typename T, int NB, int DB>
 __device__ __forceinline__ void softmax_groups(f32x16 (&x)[NB], const float *ks, bool all, uint64_t seen, int hh, float &m, float &l,
                                                f32x16 (&o)[DB], float (&p)[NB][16])
 {
-    float kc[2 * NB], vs[2 * NB], inv_vs[2 * NB];
+    float kc[2 * NB], vs[2 * NB], log_vs[2 * NB], inv_vs[2 * NB];
 #pragma unroll
     for (int g = 0; g < 2 * NB; ++g) {
         kc[g] = ks[g];
-        vs[g] = ks[4 + g];
+        vs[g] = log_vs[g] = ks[4 + g];   // (one of them is used)
         inv_vs[g] = ks[8 + g];
     }
-    softmax_blocks<sizeof(T) == 2, NB, DB>(x, kc, vs, vs, inv_vs, all, seen, hh, m, l, o, p);
+    softmax_blocks<sizeof(T) == 2, NB, DB>(x, kc, vs, log_vs, inv_vs, all, seen, hh, m, l, o, p);
 }
 // A scale as those need it: 0, which a block of zeros has, counts as 1.
-__device__ __forceinline__ float above_zero(float scale) { return scale > 0.f ? scale : 1.f; }
+__device__ __forceinline__ float not_zero(float scale) { return scale == 0.f ? 1.f : scale; }
 
 // The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
 template <int NB>

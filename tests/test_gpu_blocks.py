@@ -215,7 +215,8 @@ def test_attention_over_blocks_without_a_scale(dtype, form, impl):
 @pytest.mark.parametrize("impl", IMPLS)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("form", mu.BLOCKS)
-@pytest.mark.parametrize("d,pairs", [(64, [(1, 70), (6, 50), (40, 170), (3, 1)]), (128, [(1, 70), (6, 50), (40, 170), (3, 1)]), (128, [(150, 700), (129, 140)])])
+@pytest.mark.parametrize("d,pairs", [(64, [(1, 70), (6, 50), (40, 170), (3, 1)]), (128, [(1, 70), (6, 50), (40, 170), (3, 1)]), (128, [(150, 700), (129, 140)]),
+                                     (128, [(8, 100), (1, 33)]), (128, [(30, 333), (2, 33)]), (256, [(30, 90), (2, 33)])])
 def test_attention_does_not_see_what_is_hidden(dtype, form, impl, d, pairs):
     """NaN codes in the rest of a block, NaN scales in blocks that hold nothing, both in other pages, change nothing, bit for bit; NaN at a later
     position reaches the rows from it on alone."""
@@ -234,10 +235,27 @@ def test_attention_does_not_see_what_is_hidden(dtype, form, impl, d, pairs):
         b.pool[n + "s"].transpose(1, 2)[nothing] = math.nan
     out, lse = run_attend(b, Q)
     assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+    # scales of blocks that some rows see nothing of: no influence on those, whatever their bits
+    s = len(pairs) - 2
+    n, length = pairs[s]
+    begin = -(-(length - n + 1) // 16) * 16       # the first block behind the first row's position
+    assert begin < length
+    scales = {k: b.pool[k].clone() for k in ("Ks", "Vs")}
+    for value in (math.nan, math.inf):
+        for j in range(begin, length, 16):
+            page, at = b.place(s, j)
+            b.pool["Ks"][page, :, at // 16] = value
+            b.pool["Vs"][page, :, at // 16] = value
+        out, lse = run_attend(b, Q)
+        for r, owner, pos in b.each_row():
+            if owner != s or pos < begin:
+                assert torch.equal(out[r], clean[r]) and torch.equal(lse[r], clean_lse[r]), (r, owner, pos, value)
+            elif math.isnan(value):
+                assert torch.isnan(out[r]).all(), (r, owner, pos)
+    b.pool.update(scales)
     if form == gk.PAGES_INT8_BLOCKS:
         return
-    s = len(pairs) - 2
-    late = pairs[s][1] - pairs[s][0] // 2
+    late = length - n // 2
     page, at = b.place(s, late)
     b.pool["V"].view(torch.uint8)[page, :, at, 5] = 0x7f
     out, lse = run_attend(b, Q)
