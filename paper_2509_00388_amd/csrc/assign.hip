@@ -25,17 +25,22 @@ constexpr int kRowsAtOnce = 4096;   // rows that the workgroup tells their place
 
 __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
-// Sums up to and with this thread's value, of NW waves; sums that pass 32 bits stay at the largest number.  `part`: 17 words.
-template <int NW> __device__ __forceinline__ uint32_t scan_sat(uint32_t v, uint32_t *part, uint32_t &total)
+// Sums of two numbers of each thread up to and with this thread's, of NW waves; sums that pass 32 bits stay at the largest number.
+struct Two {
+    uint32_t a, b;
+};
+template <int NW> __device__ __forceinline__ Two scan_sat(Two v, Two *part, Two &total)   // part: NW of them
 {
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t incl = wave_scan_op(v, 0u, add_sat);
+    const Two incl{wave_scan_op(v.a, 0u, add_sat), wave_scan_op(v.b, 0u, add_sat)};
     __syncthreads();   // (the scan before is done with `part`)
     if (lane == kWave - 1) part[wv] = incl;
     __syncthreads();
-    const uint32_t sums = wave_scan_op(lane < NW ? part[lane] : 0u, 0u, add_sat);
-    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, 63);
-    return add_sat(incl, wv > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, wv - 1) : 0u);
+    const Two mine = lane < NW ? part[lane] : Two{0, 0};
+    const Two sums{wave_scan_op(mine.a, 0u, add_sat), wave_scan_op(mine.b, 0u, add_sat)};
+    auto of_lane = [](uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
+    total = {of_lane(sums.a, 63), of_lane(sums.b, 63)};
+    return {add_sat(incl.a, wv > 0 ? of_lane(sums.a, wv - 1) : 0u), add_sat(incl.b, wv > 0 ? of_lane(sums.b, wv - 1) : 0u)};
 }
 
 // The first of n ascending sums that is above i (n if none is).
@@ -59,13 +64,14 @@ __device__ __forceinline__ int slot_of(const AssignArgs &a, int s, int pos)
     return (unsigned)page < (unsigned)a.n_pages ? (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : -1;
 }
 
-// Sums of the chunks before mine, of them all, of an array that the launch before left.
-template <int NW> __device__ __forceinline__ uint32_t chunks_before(const uint32_t *sums, int chunks, int mine, uint32_t *part, uint32_t &all)
+// Sums of the chunks before mine, of them all, of two arrays that the launch before left.
+template <int NW> __device__ __forceinline__ Two chunks_before(const uint32_t *x, const uint32_t *y, int chunks, int mine, Two *part, Two &all)
 {
     const int t = threadIdx.x;
-    scan_sat<NW>(t < mine ? sums[t] : 0u, part, all);
-    const uint32_t before = all;
-    scan_sat<NW>(t < chunks ? sums[t] : 0u, part, all);
+    const Two v = t < chunks ? Two{x[t], y[t]} : Two{0, 0};
+    Two before;
+    scan_sat<NW>(t < mine ? v : Two{0, 0}, part, before);
+    scan_sat<NW>(v, part, all);
     return before;
 }
 
@@ -74,10 +80,12 @@ template <int NT, int PHASE>
 __global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sums)
 {
     constexpr int NW = NT / kWave;
-    __shared__ uint32_t part[17], by_page[NT], by_row[NT];
+    __shared__ Two part[NW];
+    __shared__ uint32_t by_page[NT], by_row[NT];
     __shared__ int first_entry[NT], length[NT];
     const int t = threadIdx.x, chunk = blockIdx.x, s = chunk * NT + t, chunks = gridDim.x;
     const bool mine = s < a.n_seqs;
+    const int here = min(NT, a.n_seqs - chunk * NT);   // sequences of the chunk
     const uint32_t cap = (uint32_t)a.table_pages << a.page_shift;
 
     uint32_t had = 0, kept = 0, fresh = 0, n_free = 0;
@@ -93,29 +101,26 @@ __global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sum
     const bool fits = fresh <= (uint32_t)a.max_rows && want <= cap;
     if (!fits) fresh = 0;
 
-    uint32_t all, asked_before = 0, taken_before = 0, given_before = 0, start_before = 0, given_all;
-    if (PHASE >= 2) asked_before = chunks_before<NW>(sums.asked, chunks, chunk, part, all);
-    const uint32_t asked = add_sat(asked_before, scan_sat<NW>(fresh, part, all));
+    Two all, before{0, 0};
+    if (PHASE >= 2) before = chunks_before<NW>(sums.asked, sums.asked, chunks, chunk, part, all);
+    const uint32_t asked = add_sat(before.a, scan_sat<NW>({fresh, 0}, part, all).a);
     if (PHASE == 1) {
-        if (t == 0) sums.asked[chunk] = all;
+        if (t == 0) sums.asked[chunk] = all.a;
         if (t == 0 && chunk == 0) sums.n_free[0] = n_free;
         return;
     }
     bool ok = fits && (fresh == 0 || asked <= (uint32_t)a.n_rows);
     const uint32_t pages = pages_of(had, a.page_shift), after = pages_of(want, a.page_shift);
     const uint32_t take = ok && after > pages ? after - pages : 0, give = ok && after < pages ? pages - after : 0;
-    uint32_t take_all;
-    uint32_t taken = scan_sat<NW>(take, part, take_all);
-    uint32_t given = scan_sat<NW>(give, part, given_all);
-    const uint32_t given_here = given_all;
+    const Two moved = scan_sat<NW>({take, give}, part, all);
+    const uint32_t taken = moved.a, given = moved.b, given_here = all.b;
     if (PHASE == 2) {
-        if (t == 0) { sums.taken[chunk] = take_all; sums.given[chunk] = given_here; }
+        if (t == 0) { sums.taken[chunk] = all.a; sums.given[chunk] = all.b; }
         return;
     }
-    if (PHASE >= 3) {
-        taken_before = chunks_before<NW>(sums.taken, chunks, chunk, part, all);
-        given_before = chunks_before<NW>(sums.given, chunks, chunk, part, given_all);
-    }
+    before = {0, 0};
+    if (PHASE >= 3) before = chunks_before<NW>(sums.taken, sums.given, chunks, chunk, part, all);
+    const uint32_t taken_before = before.a, given_before = before.b, given_all = all.b;
     const uint32_t total = min(add_sat(n_free, given_all), (uint32_t)a.n_pages);   // (more only where a page has two owners)
     ok = ok && (take == 0 || add_sat(taken_before, taken) <= total);
 
@@ -129,25 +134,22 @@ __global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sum
             __syncthreads();
             const uint32_t room = total - n_free > given_before ? total - n_free - given_before : 0;
             for (uint32_t i = t; i < min(given_here, room); i += NT) {
-                const int owner = first_above(by_page, NT, i);
-                if (owner < NT)
+                const int owner = first_above(by_page, here, i);
+                if (owner < here)
                     a.free_pages[total - 1 - (given_before + i)] = a.table[(long)(chunk * NT + owner) * a.table_pages + (first_entry[owner] + (int)i)];
             }
         }
     }
     const uint32_t rows = ok ? fresh : 0;
-    uint32_t rows_all, out_all;
-    const uint32_t rows_to = scan_sat<NW>(rows, part, rows_all);
-    scan_sat<NW>(ok ? take : 0, part, out_all);   // (those that are served come first: their sums are `taken`)
+    const uint32_t rows_to = scan_sat<NW>({rows, ok ? take : 0}, part, all).a;   // (those that are served come first: their sums are `taken`)
+    const uint32_t rows_all = all.a, out_all = all.b;
     if (PHASE == 3) {
         if (t == 0) { sums.rows[chunk] = rows_all; sums.out[chunk] = out_all; }
         return;
     }
-    uint32_t rows_total = rows_all, out_total = out_all;
-    if (PHASE == 4) {
-        start_before = chunks_before<NW>(sums.rows, chunks, chunk, part, rows_total);
-        chunks_before<NW>(sums.out, chunks, chunk, part, out_total);
-    }
+    before = {0, 0};
+    if (PHASE == 4) before = chunks_before<NW>(sums.rows, sums.out, chunks, chunk, part, all);
+    const uint32_t start_before = before.a, rows_total = all.a, out_total = all.b;
     const uint32_t len = ok ? want : had;
     if (mine) {
         a.seq_len[s] = (int32_t)len;
@@ -164,8 +166,8 @@ __global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sum
     length[t] = (int)len;
     __syncthreads();
     for (uint32_t i = t; i < out_all; i += NT) {
-        const int owner = first_above(by_page, NT, i);
-        if (owner < NT)
+        const int owner = first_above(by_page, here, i);
+        if (owner < here)
             a.table[(long)(chunk * NT + owner) * a.table_pages + (first_entry[owner] + (int)i)] = a.free_pages[total - 1 - (taken_before + i)];
     }
     if (PHASE == 0 && a.rows_here) {
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sum
         for (int r = t; r < a.n_rows; r += NT) {
             int pos = -1, slot = -1;
             if (r < (int)rows_all) {
-                const int owner = first_above(by_row, NT, (uint32_t)r);
+                const int owner = first_above(by_row, here, (uint32_t)r);
                 pos = length[owner] - (int)by_row[owner] + r;
                 slot = slot_of(a, owner, pos);
             }
@@ -183,22 +185,40 @@ __global__ __launch_bounds__(NT) void assign_kernel(AssignArgs a, AssignSums sum
     }
 }
 
-// Position and place of each row, a row a thread.
+// The sequence of row r (below the last row number) by a vote of 64 row numbers at a time, for the whole wave.
+__device__ __forceinline__ int seq_of(const AssignArgs &a, int r, int lane)
+{
+    int lo = 0, n = a.n_seqs;   // it is one of the n sequences from lo on
+    while (n > 1) {
+        const int piece = (n + kWave - 1) / kWave, ask = lo + min((lane + 1) * piece, n);   // the last of each piece
+        const int ended = (int)__popcll(__ballot(a.row_start[ask] <= r && ask < lo + n));
+        lo += ended * piece;
+        n = min(piece, n - ended * piece);
+    }
+    return lo;
+}
+
+// Position and place of each row, a row a thread.  A wave finds the sequences of its first and last row, which with many rows a sequence are the same or
+// next to one another, and each lane its own between them.
 __global__ __launch_bounds__(256) void assign_rows_kernel(AssignArgs a)
 {
-    const int r = blockIdx.x * 256 + threadIdx.x;
-    if (r >= a.n_rows) return;
+    const int r = blockIdx.x * 256 + threadIdx.x, lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(r);
+    const int rows = a.row_start[a.n_seqs];
     int pos = -1, slot = -1;
-    if (r < a.row_start[a.n_seqs]) {
-        int lo = 0;   // the first sequence that ends behind the row
-        for (int len = a.n_seqs; len > 0;) {
+    if (first < rows) {
+        int lo = seq_of(a, first, lane);
+        const int last = seq_of(a, min(first + kWave, rows) - 1, lane);
+        for (int len = last - lo; len > 0;) {   // the first that ends behind the row
             const int half = len >> 1;
             if (a.row_start[lo + half + 1] <= r) { lo += half + 1; len -= half + 1; }
             else len = half;
         }
-        pos = a.seq_len[lo] - a.row_start[lo + 1] + r;
-        slot = slot_of(a, lo, pos);
+        if (r < rows) {
+            pos = a.seq_len[lo] - a.row_start[lo + 1] + r;
+            slot = slot_of(a, lo, pos);
+        }
     }
+    if (r >= a.n_rows) return;
     if (a.positions) a.positions[r] = pos;
     if (a.slots) a.slots[r] = slot;
 }
