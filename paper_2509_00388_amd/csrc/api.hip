@@ -367,7 +367,7 @@ struct AttendPlan {
 
 static_assert(kBlocksFp8 == GRAPHKV_PAGES_FP8_BLOCKS && kBlocksInt8 == GRAPHKV_PAGES_INT8_BLOCKS, "");
 
-bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
+bool plan_attend(const graphkv_paged_params *p, AttendPlan &A, bool cross = false)   // (cross: no more scratch memory than without)
 {
     if (!paged_ok(p)) return false;
     if (p->n_q_heads < p->n_kv_heads || p->n_q_heads > 65535 || p->n_q_heads % p->n_kv_heads) return false;
@@ -390,7 +390,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A)
         // (and so are the key tiles of all sequences and heads, at least 128 keys each)
         const int64_t tokens = (int64_t)p->table_pages * p->page_tokens;
         if ((tokens + 127) / 128 * p->n_kv_heads * (int64_t)p->n_seqs > INT32_MAX) return false;
-        A.fp = few_plan(b, p->dtype, p->page_format, A.G);
+        A.fp = few_plan(b, p->dtype, p->page_format, A.G, cross);
         A.few_slots = align_up(join_record_bytes(A.fp.join));
         A.total = A.few_slots + align_up(join_slot_bytes(A.fp.join));
     }
@@ -416,7 +416,7 @@ int32_t run_attend(const graphkv_paged_params *p, bool cross, const void *Q, con
                    void *ws, size_t ws_bytes, void *stream)
 {
     AttendPlan A;
-    if (!plan_attend(p, A)) return GRAPHKV_EINVAL;
+    if (!plan_attend(p, A, cross)) return GRAPHKV_EINVAL;
     AttendArgs a{};
     if (!take_strides(p, p->n_q_heads, p->row_stride, p->head_stride, false, a.q_row, a.q_head) ||
         !take_strides(p, p->n_q_heads, p->out_row_stride, p->out_head_stride, true, a.o_row, a.o_head))
@@ -453,7 +453,8 @@ int32_t run_attend(const graphkv_paged_params *p, bool cross, const void *Q, con
         GKV_LAUNCH(GRAPHKV_K_ATTEND_MANY, A.mp.wide ? launch_attend_wide(a, A.mp, p->page_format, cross, st)
                                                     : launch_attend_many(a, A.mp, p->dtype, p->page_format, cross, st));
     }
-    GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, A.mp.join, p->dtype, st));
+    if ((A.few && !A.fp.whole) || (A.many && !A.mp.single))   // (otherwise no block of rows has several parts)
+        GKV_LAUNCH(GRAPHKV_K_ATTEND_JOIN, launch_attend_join(a, A.fp.join, A.mp.join, p->dtype, st));
     return GRAPHKV_OK;
 }
 

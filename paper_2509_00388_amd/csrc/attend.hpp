@@ -113,12 +113,9 @@ constexpr int kMostFewWorkgroups = 512;   // two a compute unit
 struct FewPlan {
     JoinPlan join;
     int tile_keys;
+    int whole;        // no pair is split: stretches are of pairs, and nothing is left to be joined
 };
 __device__ __forceinline__ bool has_few(const SeqRows &q, int G) { return q.n > 0 && q.n * (long)G <= kFewRows; }
-__device__ __forceinline__ uint32_t few_tiles(const SeqRows &q, const AttendArgs &a, const FewPlan &p)   // of a head
-{
-    return has_few(q, a.G) ? max(1, (q.len + p.tile_keys - 1) / p.tile_keys) : 0;
-}
 
 // Many rows: blocks of R stacked rows of a head, and of the key tiles that each sees so many units of `step` tiles.  The units of
 // all (sequence, head, block) are cut into equal stretches as above.  A causal chunk's blocks see more and more keys; so that the work
@@ -131,6 +128,7 @@ struct ManyPlan {
     int block_rows, tile_keys, step;
     int leave_few;    // sequences of few rows are the other kernel's
     int wide;         // blocks of 256 rows (attend_wide.hpp)
+    int single;       // a block has one unit: none is split
 };
 struct ManySeq {
     int rows, blocks;        // stacked
@@ -202,7 +200,7 @@ __device__ __forceinline__ bool next_part(const AttendArgs &a, const ManyPlan &p
 
 // ---- launchers ------------------------------------------------------------------------------------------
 bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
-FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G);
+FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G, bool cross);
 ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);   // no workgroups: more units than 31 bits count
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, bool cross, hipStream_t st);
 // (`cross`: rows see all of their sequence.  The kernels of each kind are compiled in files of their own: these, blocks_attend.hip, cross_*.hip.)
