@@ -81,14 +81,12 @@ __device__ int find_share(int n_seqs, uint32_t &total, uint32_t &before, uint32_
 }
 
 // Equal stretches of `total` units for n workgroups: the first unit of the w-th, and the one that takes a unit.
-__device__ __forceinline__ uint32_t stretch_first(uint32_t total, int w, int n) { return (uint32_t)((uint64_t)total * w / n); }
+// (With 32 bits, w <= n < 2^16: total = q n + r, so that total w / n = q w + r w / n.)
+__device__ __forceinline__ uint32_t stretch_first(uint32_t total, uint32_t w, uint32_t n) { return total / n * w + total % n * w / n; }
 __device__ __forceinline__ int stretch_owner(uint32_t total, uint32_t unit, int n)
 {
     return min((int)((((uint64_t)unit + 1) * n - 1) / total), n - 1);
 }
-
-// stretch_first() with 32 bits, for few workgroups: total = q n + r, so that total w / n = q w + r w / n.
-__device__ __forceinline__ uint32_t few_first(uint32_t total, uint32_t w, uint32_t n) { return total / n * w + total % n * w / n; }
 
 // What a workgroup leaves of a block of rows that others hold parts of too: every workgroup has two slots, for the part its
 // stretch begins with and the part it ends with, and a record of a block whose first part it holds.  The other parts of
@@ -126,6 +124,7 @@ __device__ __forceinline__ bool has_few(const SeqRows &q, int G) { return q.n > 
 struct ManyPlan {
     JoinPlan join;
     int block_rows, tile_keys, step;
+    int block_shift, unit_shift;   // log2 of block_rows and of a unit's tile_keys * step keys
     int leave_few;    // sequences of few rows are the other kernel's
     int wide;         // blocks of 256 rows (attend_wide.hpp)
     int single;       // a block has one unit: none is split
@@ -142,8 +141,7 @@ __device__ __forceinline__ uint32_t many_units(const SeqRows &q, int rows, int k
 {
     const uint32_t end = (uint32_t)(k + 1) * p.block_rows;
     const int sees = CROSS ? q.len : q.len - q.n + (int)(((whole ? end : min(end, (uint32_t)rows)) - 1) / (uint32_t)a.G) + 1;
-    const uint32_t keys = (uint32_t)p.tile_keys * p.step;
-    return sees <= (int)keys ? 1u : ((uint32_t)sees + keys - 1) / keys;
+    return sees <= 1 ? 1u : ((uint32_t)sees + (1u << p.unit_shift) - 1) >> p.unit_shift;
 }
 template <bool CROSS>
 __device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &a, const ManyPlan &p)
@@ -151,7 +149,7 @@ __device__ __forceinline__ ManySeq many_seq(const SeqRows &q, const AttendArgs &
     ManySeq m{};
     if (q.n <= 0 || (p.leave_few && has_few(q, a.G))) return m;
     m.rows = q.n * a.G;
-    m.blocks = (m.rows + p.block_rows - 1) / p.block_rows;
+    m.blocks = (m.rows + p.block_rows - 1) >> p.block_shift;
     if (m.blocks > 1) m.pair = many_units<CROSS>(q, m.rows, 0, true, a, p) + many_units<CROSS>(q, m.rows, m.blocks - 1, true, a, p) + (CROSS ? 0 : 2);
     if (m.blocks & 1) m.middle = many_units<CROSS>(q, m.rows, m.blocks / 2, false, a, p);
     m.per_head = m.blocks / 2 * m.pair + m.middle;

@@ -31,6 +31,8 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
         units = (blocks / 2 + b.n_seqs) * (2 * (cap / ((long)p.tile_keys * p.step) + 1) + 2) * b.H;
         if (units <= INT32_MAX || p.tile_keys * p.step >= 1 << 29) break;
     }
+    p.block_shift = __builtin_ctz((unsigned)p.block_rows);
+    p.unit_shift = __builtin_ctz((unsigned)(p.tile_keys * p.step));
     p.single = cap <= (long)p.tile_keys * p.step;
     const int most = p.wide ? 256 : 512;   // one or two workgroups a compute unit
     p.join.n_wg = units > INT32_MAX ? 0 : units < most ? (int)units : most;
