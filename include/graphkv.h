@@ -308,7 +308,8 @@ int32_t graphkv_compress_static(const graphkv_params *p, const void *Kc, const v
  * adds behind tokens which a block holds already keep the block's scale if it is as large as theirs would be;
  * otherwise it becomes theirs, and the codes of the tokens before them become those nearest to code * old scale /
  * new scale (for e4m3 the least bits of small values go, for integers each such step adds at most half of one of the new scale).
- * A scale does not shrink while its block grows, not even where tokens that had asked for it were taken back.
+ * A scale does not shrink while its block grows, not even where tokens that had asked for it were taken back.  (Pools filled by
+ * other means: attention takes scales that are 0 or above, and codes that are 0 where the scale is.)
  */
 enum { GRAPHKV_PAGES_PLAIN = 0, GRAPHKV_PAGES_FP8 = 1, GRAPHKV_PAGES_INT8 = 2,
        GRAPHKV_PAGES_FP8_BLOCKS = 5, GRAPHKV_PAGES_INT8_BLOCKS = 6 };
@@ -378,7 +379,8 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  * memory is needed: by the scalar kernel, and without rows or sequences.
  * Softmax statistics and sums are held in 32 bits.  With bf16 rows the weights (times the
  * values' scales, of 8-bit pages) are rounded to bf16 for the product with the values; where the kernel
- * for few rows reads plain pages, to two bf16 numbers each, which keep 15 bits.  (Sums of values
+ * for few rows reads plain pages, to two bf16 numbers each, which keep 15 bits.  (With pages in blocks a weight and the scale of its value are one
+ * exponential, whose argument is rounded to 32 bits.)  (Sums of values
  * beyond 2^100 may leave the range of 32 bits.)  A row that sees nothing, or
  * nothing but logits of -infinity, has out = 0 and lse = -infinity.  What lies in places that a row does not see (later
  * positions, the rest of a page) has no influence on it, whatever its bits.

@@ -12,7 +12,9 @@
 // Up to 1024 sequences a workgroup does all this, a sequence a thread, with three scans; beyond, workgroups of 1024 each go as far as they get
 // without the others' sums, leave theirs, and begin anew in the next launch: four of them, whatever the number.  Page numbers
 // and rows are dealt to the threads one by one, whoever's they are, and find their sequence in the sums, which lie in the LDS.  Few rows
-// are told their places in the same launch, many in one of their own.  Nothing but latency: a batch's numbers are a few kilobytes.
+// are told their places in the same launch, many in one of their own.  Nothing but latency: a batch's numbers are a few kilobytes.  A token each of 64
+// sequences 4.0 us, 1000 sequences of which 111 end and are followed by prompts, 4400 pages that move and 126000 rows, 9.0 + 4.0, a prompt of 120000 rows
+// 4.2 + 2.9; a call takes the host 9.
 #include "kernels.hpp"
 #include "paged.hpp"
 
@@ -236,8 +238,8 @@ hipError_t launch_assign(const AssignArgs &args, void *scratch, hipStream_t st)
     const int chunks = chunks_of(a.n_seqs);
     if (chunks <= 1) {
         a.rows_here = maps && a.n_rows <= kRowsAtOnce;
-        // (a workgroup of 256 threads is done sooner with its barriers: a turn of 64 sequences 4.3 us of 5.4; of 1024 with thousands of pages, which few
-        // sequences ask for where they have many rows)
+        // (256 threads are done sooner with their barriers, 1024 with thousands of pages, which few sequences ask for where they have many rows: one of
+        // 120000 rows 8.1 / 5.4 us)
         if (a.n_seqs <= 256 && a.n_rows >> a.page_shift <= 256) assign_kernel<256, 0><<<1, 256, 0, st>>>(a, AssignSums{});
         else assign_kernel<kChunk, 0><<<1, kChunk, 0, st>>>(a, AssignSums{});
     } else {
