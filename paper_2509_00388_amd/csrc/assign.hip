@@ -22,8 +22,7 @@ namespace gkv {
 
 namespace {
 
-constexpr int kChunk = 1024;        // sequences of a workgroup
-constexpr int kRowsAtOnce = 4096;   // rows that the workgroup tells their places itself
+constexpr int kChunk = 1024;   // sequences of a workgroup
 
 __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
@@ -237,10 +236,13 @@ hipError_t launch_assign(const AssignArgs &args, void *scratch, hipStream_t st)
     const bool maps = (a.positions || a.slots) && a.n_rows > 0;
     const int chunks = chunks_of(a.n_seqs);
     if (chunks <= 1) {
-        a.rows_here = maps && a.n_rows <= kRowsAtOnce;
-        // (256 threads are done sooner with their barriers, 1024 with thousands of pages, which few sequences ask for where they have many rows: one of
-        // 120000 rows 8.1 / 5.4 us)
-        if (a.n_seqs <= 256 && a.n_rows >> a.page_shift <= 256) assign_kernel<256, 0><<<1, 256, 0, st>>>(a, AssignSums{});
+        // (256 threads are done sooner with their barriers, 1024 with thousands of pages, which few sequences ask for where they have many rows: 64 sequences with
+        // a row each 4.2 / 5.0 us, one of 4000 rows, of 16000 and of 60000 in pages of 16 5.4 / 5.5, 6.0 / 6.2, 8.2 / 7.0)
+        const bool small = a.n_seqs <= 256 && a.n_rows >> a.page_shift <= 1024;
+        // (rows told here or by a launch of their own: 64 sequences of 4, 16 and 32 rows 4.2 / 5.4, 6.0 / 6.1, 8.3 / 6.4 us, 1000 of 1, 2 and 4 rows 5.9 / 8.0,
+        // 6.8 / 8.1, 8.7 / 7.9)
+        a.rows_here = maps && a.n_rows <= (small ? 1024 : 2048);
+        if (small) assign_kernel<256, 0><<<1, 256, 0, st>>>(a, AssignSums{});
         else assign_kernel<kChunk, 0><<<1, kChunk, 0, st>>>(a, AssignSums{});
     } else {
         uint32_t *w = reinterpret_cast<uint32_t *>(scratch);
