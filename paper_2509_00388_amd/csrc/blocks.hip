@@ -5,17 +5,16 @@
 // rounded again, round(code * old / new): a power of two apart for e4m3, in 64 bits for integers.
 //
 // A wave or a workgroup takes a block of a head: the largest magnitude of its new rows, then their codes; rows stay in registers between the two where
-// they are few enough, else they are read again.  Blocks are found by their first new row: a workgroup looks at a stretch of rows for those that
-// begin one.  Bound by memory where rows are many: 20000 bf16 rows of eight heads of 128 to fp8 in blocks of 64 in 28 us, 4.4 TB/s; 2055 fp32 rows of
-// sixteen heads of 64 to int8 in blocks of 16 in 12 us, a round of waves; a token each of 64 sequences
-// in 4.5 us, a chain of look-ups and loads.
+// they are few enough, else they are read again.  Which block it is follows from the blocks that the sequences before have new rows in: a lane counts
+// a sequence's.  Bound by memory where rows are many: 20000 bf16 rows of eight heads of 128 to fp8 in blocks of 64 in 28 us, 4.4 TB/s; 2055 fp32 rows of
+// sixteen heads of 64 to int8 in blocks of 16 in 11 us, a round of waves; a token each of 64 sequences in 4.2 us, a chain of look-ups and loads.  Blocks found from rows that
+// begin one cost 64 sequences of 8 rows 10.7 us of a call where these cost 6.8, of 64 rows in blocks of 128 76 and 12.5.
 #include "kernels.hpp"
 #include "paged.hpp"
 
 namespace gkv {
 
 namespace {
-
 
 // The largest of a wave's numbers that are not below 0, in all lanes.
 __device__ __forceinline__ float wave_largest(float x) { return __uint_as_float(wave_max_u32(__float_as_uint(x))); }
@@ -66,7 +65,7 @@ struct BlocksWrite {
     long row_stride, head_stride;
     void *Kpages, *Vpages;
     float *Kscale, *Vscale;
-    int group, stretch;   // lanes of a row, rows that a workgroup looks at
+    int group;   // lanes of a row
 };
 
 // A block of a head is WAVES waves' work: of one, so that four heads share a workgroup, or of all four.  HELD: pieces of each tensor that a thread
@@ -83,100 +82,110 @@ __global__ __launch_bounds__(256) void blocks_write_kernel(PagedBatch b, BlocksW
     const int tokens = 1 << b.scale_shift;
     const T *K = reinterpret_cast<const T *>(w.K) + h * w.head_stride, *V = reinterpret_cast<const T *>(w.V) + h * w.head_stride;
 
-    const int last = min((int)(blockIdx.x + 1) * w.stretch, b.n_rows);
-    SeqRows q{0, 0, 0};
-    int s = -1, turn = blockIdx.z;   // of the blocks that begin in the stretch, every gridDim.z-th from there on is this workgroup's
-    for (int row = blockIdx.x * w.stretch; row < last;) {
-        if (s < 0 || row >= q.row0 + q.n) {
-            s = seq_of_row(b, row, lane);
-            if (s >= b.n_seqs) break;
-            q = seq_rows(b, s);
+    // Block number blockIdx.x of those with new rows: a lane counts those of a sequence, 64 sequences at a time (four a lane are no faster).
+    uint32_t number = blockIdx.x;
+    int s = 0, row0 = 0, lo = 0, len = 0, which = -1;   // sequence, row of its position 0 (were it there), new positions, which of its blocks
+    for (int from = 0; from < b.n_seqs; from += kWave) {
+        const int x = from + lane;
+        SeqRows q{0, 0, 0};
+        if (x < b.n_seqs) q = seq_rows(b, x);
+        const int start = max(q.len - q.n, 0);   // (more rows than the sequence is long: the first have no place)
+        const uint32_t has = q.n > 0 && q.len > 0 ? ((q.len - 1) >> b.scale_shift) - (start >> b.scale_shift) + 1 : 0;
+        const uint32_t incl = wave_scan_op(has, 0u, [](uint32_t l, uint32_t r) { return l + r; });
+        const uint64_t above = __ballot(incl > number);
+        if (above == 0) {
+            number -= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
+            continue;
         }
-        const int i = row - q.row0, pos = q.len - q.n + i;
-        if (i < 0 || i >= q.n) { ++row; s = -1; continue; }
-        if (pos < 0) { row += min(-pos, q.n - i); continue; }
-        const int inside = pos & (tokens - 1);
-        const int rest = min(tokens - inside, q.len - pos);   // rows up to the block's end or the sequence's
-        const int first = row;
-        row += rest;
-        if (inside > 0 && i > 0) continue;   // the block's first new row is another's
-        if (turn-- > 0) continue;
-        turn = gridDim.z - 1;
-        const int page = page_of(b, s, pos);
-        if (page < 0) continue;
+        const int l = __builtin_ctzll(above);
+        auto of_lane = [l](int v) { return __builtin_amdgcn_readlane(v, l); };
+        s = from + l;
+        row0 = of_lane(q.row0 + q.n - q.len);
+        lo = of_lane(start);
+        len = of_lane(q.len);
+        which = (int)(number - (uint32_t)of_lane((int)(incl - has)));
+        break;
+    }
+    // (The grid has room for blocks that a sequence may begin in their middle; sums of row numbers that do not ascend may pass 32 bits.)
+    if (which < 0 || which > ((len - 1) >> b.scale_shift) - (lo >> b.scale_shift)) return;
+    const int begin = ((lo >> b.scale_shift) + which) << b.scale_shift;   // the block's first position
+    const int pos = max(begin, lo), inside = pos - begin, rest = min(begin + tokens, len) - pos, first = row0 + pos;
+    const int page = raw_page(b, s, pos);
+    auto row_of = [&](const T *x, int r) { return reinterpret_cast<const uint4 *>(x + (first + r) * w.row_stride); };
+    const bool held = rest <= HELD * step && pieces <= w.group;
+    const int turns = (rest + step - 1) / step;
+    uint4 kv[HELD], vv[HELD];
+    if (held) {
+#pragma unroll
+        for (int t = 0; t < HELD; ++t) {   // (a turn or lane without a piece takes another's: neither largest nor code changes by that)
+            const int r = min(mine + min(t, turns - 1) * step, rest - 1), p = min(at, pieces - 1);
+            kv[t] = row_of(K, r)[p];
+            vv[t] = row_of(V, r)[p];
+        }
+    }
+    if (!is_page(b, page)) return;
 
-        const int base = pool_row(b, page, h, pos - inside), block = base >> b.scale_shift;
-        const float kb = inside > 0 ? w.Kscale[block] : 0.f, vb = inside > 0 ? w.Vscale[block] : 0.f;
-        char *kto = reinterpret_cast<char *>(w.Kpages) + (long)base * b.d, *vto = reinterpret_cast<char *>(w.Vpages) + (long)base * b.d;
-        auto row_of = [&](const T *x, int r) { return reinterpret_cast<const uint4 *>(x + (first + r) * w.row_stride); };
-        float ks, vs, kinv, vinv;
-        // The block's scales, from its new rows' largest magnitudes; codes that are there to the new ones.
-        auto settle = [&](float ka, float va) {
-            ka = wave_largest(ka);
-            va = wave_largest(va);
-            if constexpr (WAVES > 1) {
-                __syncthreads();   // (the block before is done with them)
-                if (lane == 0) { tops[0][wv] = ka; tops[1][wv] = va; }
-                __syncthreads();
-                ka = fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3]));
-                va = fmaxf(fmaxf(tops[1][0], tops[1][1]), fmaxf(tops[1][2], tops[1][3]));
-            }
-            ks = fmaxf(kb, scale_of<FORM>(ka));
-            vs = fmaxf(vb, scale_of<FORM>(va));
-            kinv = ks > 0.f ? 1.f / ks : 0.f;
-            vinv = vs > 0.f ? 1.f / vs : 0.f;
-            if (tid == 0) { w.Kscale[block] = ks; w.Vscale[block] = vs; }
-            const int old = kb < ks || vb < vs ? inside * (b.d / 16) : 0;   // (the codes before the first new row are a run of them)
-#pragma unroll 1
-            for (int p = tid; p < old; p += THREADS) {
-                if (kb < ks) { uint4 *x = reinterpret_cast<uint4 *>(kto) + p; *x = encode_again<FORM>(*x, kb, ks); }
-                if (vb < vs) { uint4 *x = reinterpret_cast<uint4 *>(vto) + p; *x = encode_again<FORM>(*x, vb, vs); }
-            }
-            kto += (long)inside * b.d;
-            vto += (long)inside * b.d;
-        };
-        if (rest <= HELD * step && pieces <= w.group) {
-            const int turns = (rest + step - 1) / step;
-            uint4 kv[HELD], vv[HELD];
-            float ka = 0.f, va = 0.f;
-#pragma unroll
-            for (int t = 0; t < HELD; ++t) {   // (a turn or lane without a piece takes another's: neither largest nor code changes by that)
-                const int r = min(mine + min(t, turns - 1) * step, rest - 1), p = min(at, pieces - 1);
-                kv[t] = row_of(K, r)[p];
-                vv[t] = row_of(V, r)[p];
-            }
-#pragma unroll
-            for (int t = 0; t < HELD; ++t) {
-                ka = largest_of<T>(kv[t], ka);
-                va = largest_of<T>(vv[t], va);
-            }
-            settle(ka, va);
-#pragma unroll
-            for (int t = 0; t < HELD; ++t)   // (what was unpacked for the largest is not kept: it would take the registers of half the waves)
-                asm volatile("" : "+v"(kv[t].x), "+v"(kv[t].y), "+v"(kv[t].z), "+v"(kv[t].w), "+v"(vv[t].x), "+v"(vv[t].y), "+v"(vv[t].z), "+v"(vv[t].w));
-#pragma unroll
-            for (int t = 0; t < HELD; ++t)
-                if (t < turns) {
-                    const int to = min(mine + t * step, rest - 1) * b.d + min(at, pieces - 1) * PER;
-                    put_codes<T, FORM>(kto + to, kv[t], ks, kinv);
-                    put_codes<T, FORM>(vto + to, vv[t], vs, vinv);
-                }
-        } else {
-            float ka = 0.f, va = 0.f;
-            for (int r = mine; r < rest; r += step)
-#pragma unroll 1
-                for (int p = at; p < pieces; p += w.group) {
-                    ka = largest_of<T>(row_of(K, r)[p], ka);
-                    va = largest_of<T>(row_of(V, r)[p], va);
-                }
-            settle(ka, va);
-            for (int r = mine; r < rest; r += step)
-#pragma unroll 1
-                for (int p = at; p < pieces; p += w.group) {
-                    put_codes<T, FORM>(kto + (long)r * b.d + p * PER, row_of(K, r)[p], ks, kinv);
-                    put_codes<T, FORM>(vto + (long)r * b.d + p * PER, row_of(V, r)[p], vs, vinv);
-                }
+    const int base = pool_row(b, page, h, begin), block = base >> b.scale_shift;
+    const float kb = inside > 0 ? w.Kscale[block] : 0.f, vb = inside > 0 ? w.Vscale[block] : 0.f;
+    char *kto = reinterpret_cast<char *>(w.Kpages) + (long)base * b.d, *vto = reinterpret_cast<char *>(w.Vpages) + (long)base * b.d;
+    float ks, vs, kinv, vinv;
+    // The block's scales, from its new rows' largest magnitudes; codes that are there to the new ones.
+    auto settle = [&](float ka, float va) {
+        ka = wave_largest(ka);
+        va = wave_largest(va);
+        if constexpr (WAVES > 1) {
+            if (lane == 0) { tops[0][wv] = ka; tops[1][wv] = va; }
+            __syncthreads();
+            ka = fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3]));
+            va = fmaxf(fmaxf(tops[1][0], tops[1][1]), fmaxf(tops[1][2], tops[1][3]));
         }
+        ks = fmaxf(kb, scale_of<FORM>(ka));
+        vs = fmaxf(vb, scale_of<FORM>(va));
+        kinv = ks > 0.f ? 1.f / ks : 0.f;
+        vinv = vs > 0.f ? 1.f / vs : 0.f;
+        if (tid == 0) { w.Kscale[block] = ks; w.Vscale[block] = vs; }
+        const int old = kb < ks || vb < vs ? inside * (b.d / 16) : 0;   // (the codes before the first new row are a run of them)
+#pragma unroll 1
+        for (int p = tid; p < old; p += THREADS) {
+            if (kb < ks) { uint4 *x = reinterpret_cast<uint4 *>(kto) + p; *x = encode_again<FORM>(*x, kb, ks); }
+            if (vb < vs) { uint4 *x = reinterpret_cast<uint4 *>(vto) + p; *x = encode_again<FORM>(*x, vb, vs); }
+        }
+        kto += (long)inside * b.d;
+        vto += (long)inside * b.d;
+    };
+    if (held) {
+        float ka = 0.f, va = 0.f;
+#pragma unroll
+        for (int t = 0; t < HELD; ++t) {
+            ka = largest_of<T>(kv[t], ka);
+            va = largest_of<T>(vv[t], va);
+        }
+        settle(ka, va);
+#pragma unroll
+        for (int t = 0; t < HELD; ++t)   // (what was unpacked for the largest is not kept: it would take the registers of half the waves)
+            asm volatile("" : "+v"(kv[t].x), "+v"(kv[t].y), "+v"(kv[t].z), "+v"(kv[t].w), "+v"(vv[t].x), "+v"(vv[t].y), "+v"(vv[t].z), "+v"(vv[t].w));
+#pragma unroll
+        for (int t = 0; t < HELD; ++t)
+            if (t < turns) {
+                const int to = min(mine + t * step, rest - 1) * b.d + min(at, pieces - 1) * PER;
+                put_codes<T, FORM>(kto + to, kv[t], ks, kinv);
+                put_codes<T, FORM>(vto + to, vv[t], vs, vinv);
+            }
+    } else {
+        float ka = 0.f, va = 0.f;
+        for (int r = mine; r < rest; r += step)
+#pragma unroll 1
+            for (int p = at; p < pieces; p += w.group) {
+                ka = largest_of<T>(row_of(K, r)[p], ka);
+                va = largest_of<T>(row_of(V, r)[p], va);
+            }
+        settle(ka, va);
+        for (int r = mine; r < rest; r += step)
+#pragma unroll 1
+            for (int p = at; p < pieces; p += w.group) {
+                put_codes<T, FORM>(kto + (long)r * b.d + p * PER, row_of(K, r)[p], ks, kinv);
+                put_codes<T, FORM>(vto + (long)r * b.d + p * PER, row_of(V, r)[p], vs, vinv);
+            }
     }
 }
 
@@ -188,15 +197,13 @@ hipError_t launch_blocks_write(const PagedBatch &b, int dtype, int form, const v
     const int pieces = b.d / (dtype == 0 ? 4 : 8);
     int group = 1;
     while (group < pieces && group < kWave) group <<= 1;
-    // Stretches of a block's tokens, in which a long sequence begins one block; where sequences have fewer rows than that, or the rows are few
-    // altogether, a row each.
+    const BlocksWrite w{K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, group};
     const int tokens = 1 << b.scale_shift, most = b.max_rows < tokens ? b.max_rows : tokens;   // new rows of a block
-    const bool single = b.max_rows < tokens || (long)b.n_rows * b.H <= 4096;
-    const BlocksWrite w{K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, group, single ? 1 : tokens};
     const int at_once = kWave / group;   // rows that a wave takes at once
-    const bool one_wave = most <= 8 * at_once;
-    // (Two workgroups a stretch where several sequences may begin a block each in it.)
-    const dim3 grid((b.n_rows + w.stretch - 1) / w.stretch, one_wave ? (b.H + 3) / 4 : b.H, !single && b.n_seqs > 1 ? 2 : 1);
+    const bool one_wave = most <= 8 * at_once;   // (400 rows of 128 bf16: blocks of 32 in 9.9 us by a wave, 13.3 by four; of 64, twice as many turns, 22.2 and 12.6)
+    // n rows of a sequence lie in (n - 2) / tokens + 2 blocks at most, and in n.
+    const long blocks = b.n_rows / tokens + 2l * b.n_seqs;
+    const dim3 grid(blocks < b.n_rows ? (int)blocks : b.n_rows, one_wave ? (b.H + 3) / 4 : b.H);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(b, w); return hipGetLastError(); };
     auto with_size = [&](auto type, auto f) {
         using T = decltype(type);

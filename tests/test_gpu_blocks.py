@@ -127,6 +127,44 @@ def test_many_sequences_and_rows(dtype):
         check_write(b, spread(b, 8), spread(b, 8))
 
 
+def test_as_many_blocks_as_rows_can_lie_in():
+    """Rows that begin with a block's last token and end with one's first; calls that do not tell how many rows a sequence has."""
+    say("as many blocks as rows can lie in")
+    for n, seqs in ((1, 130), (2, 130), (18, 100), (34, 65), (18, 1), (2, 1)):
+        for max_rows in (n, n * seqs):
+            b = mu.Batch([(n, 15 + n + 16 * (s % 3)) for s in range(seqs)], form=gk.PAGES_INT8_BLOCKS, block=16, H=5, d=64, ps=32, max_rows=max_rows)
+            check_write(b, spread(b, 5), spread(b, 5))
+
+
+@pytest.mark.parametrize("form", mu.BLOCKS)
+def test_writes_with_numbers_of_any_content(form):
+    """Lengths, row numbers and page numbers without any sense: nothing around the pools is touched."""
+    say(f"writes with numbers of any content form={form}")
+    g = torch.Generator().manual_seed(17)
+    H, d, ps, pages, block = 3, 64, 32, 40, 16
+    pool = pages * H * ps * d
+    for n_seqs, rows in ((1, 9), (70, 300), (200, 1)):
+        p = gk.PagedParams(n_kv_heads=H, head_dim=d, page_tokens=ps, n_pages=pages, n_seqs=n_seqs, table_pages=6, n_rows=rows, page_format=form,
+                           scale_tokens=block)
+        x = torch.randn(rows, H, d, generator=g).to(torch.bfloat16).cuda()
+        for kind in range(4):
+            codes = [torch.full((pool + 512,), 77, dtype=torch.uint8, device="cuda") for _ in range(2)]
+            scales = [torch.full((pages * H * ps // block + 128,), 77.0, device="cuda") for _ in range(2)]
+            big = [3, 2 ** 31 - 1, 2 ** 10, 2 ** 20][kind]
+            numbers = [torch.randint(-big, big, shape, generator=g).int().cuda() for shape in ((n_seqs, 6), (n_seqs,), (n_seqs + 1,))]
+            table, length, start = numbers
+            if kind == 2:
+                table = torch.randint(0, pages, (n_seqs, 6), generator=g).int().cuda()
+            t = torch.int8 if form == gk.PAGES_INT8_BLOCKS else torch.float8_e4m3fn
+            K, V = (c[256:-256].view(t).view(pages, H, ps, d) for c in codes)
+            Ks, Vs = (c[64:-64].view(pages, H, ps // block) for c in scales)
+            gk.graphkv_cache_write(p, x, x, K, V, table, length, start, Ks, Vs)
+            for c in codes:
+                assert (c[:256] == 77).all() and (c[-256:] == 77).all()
+            for c in scales:
+                assert (c[:64] == 77).all() and (c[-64:] == 77).all()
+
+
 def test_codes_next_to_borders():
     """Values in the middle between two codes and one step of their type next to it, new ones and ones that are rounded again."""
     say("codes next to borders")
