@@ -60,8 +60,8 @@ template <typename T, int FORM, int D, bool CROSS>
 hipError_t go_few(const AttendArgs &a, const FewPlan &pl, hipStream_t st)
 {
     constexpr int NB = blocks_of<T, FORM, D>();
-    using P = WavePlace<T, FORM, D, NB>;
-    const int tiles = 4 * P::kBytes + 32 * P::kPitch;
+    using P = WavePlace<TileType<T, FORM>, FORM, D, NB>;
+    const int tiles = 4 * P::kBytes + (in_thirds<T, FORM>() ? 3 : 1) * 32 * P::kPitch;
     const int joined = (256 + 4 * pl.join.slot_rows * (D + 4) + pl.join.slot_rows) * 4;
     const int lds = tiles > joined ? tiles : joined;
     auto kernel = few_kernel<T, FORM, D, NB, CROSS>();

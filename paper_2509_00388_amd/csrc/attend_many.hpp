@@ -56,7 +56,7 @@ template <typename T, int FORM, int D, int RG, bool CROSS>
 hipError_t go_many_rows(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
 {
     constexpr int KEYS = many_tile_keys<T, D>(), NB = KEYS * RG / 128;
-    using L = Tile<T, FORM, D, KEYS, 256>;
+    using L = Tile<TileType<T, FORM>, FORM, D, KEYS, 256>;
     const int tiles = 2 * (KEYS * (L::kKeyPitch + L::kValPitch) + scale_bytes(FORM, KEYS));
     const int joined = RG == 4 ? 0 : (64 * RG + 32 * RG * (D + 4)) * 4;
     const int lds = tiles > joined ? tiles : joined;
