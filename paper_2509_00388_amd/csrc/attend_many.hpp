@@ -26,6 +26,9 @@ namespace {
 // softmax_blocks() takes it).
 constexpr int scale_bytes(int form, int keys) { return form == kPagesPlain ? 0 : in_blocks(form) ? 64 : 2 * keys * 4; }
 
+// Bytes of the third part of a wave's queries in the LDS (attend_many.inc).
+template <int D> constexpr int kThirdBytes = 32 * (2 * D + 16);
+
 #define GKV_KERNEL attend_many_kernel   // pages of rows, plain or with a scale each
 #define GKV_CROSS false
 #include "attend_many.inc"
@@ -57,7 +60,7 @@ hipError_t go_many_rows(const AttendArgs &a, const ManyPlan &pl, hipStream_t st)
 {
     constexpr int KEYS = many_tile_keys<T, D>(), NB = KEYS * RG / 128;
     using L = Tile<TileType<T, FORM>, FORM, D, KEYS, 256>;
-    const int tiles = 2 * (KEYS * (L::kKeyPitch + L::kValPitch) + scale_bytes(FORM, KEYS));
+    const int tiles = 2 * (KEYS * (L::kKeyPitch + L::kValPitch) + scale_bytes(FORM, KEYS)) + (in_thirds<T, FORM>() && D >= 128 ? 4 * kThirdBytes<D> : 0);
     const int joined = RG == 4 ? 0 : (64 * RG + 32 * RG * (D + 4)) * 4;
     const int lds = tiles > joined ? tiles : joined;
     auto kernel = many_kernel<T, FORM, D, NB, RG, CROSS>();

@@ -15,8 +15,9 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // Rows of 32 bits over codes in blocks, which bf16 holds as they are: queries and weights are cut into three bf16 parts of eight bits each, which
-// are all that they have, and the products are three of the bf16 instruction, sixteen times as fast as that of 32 bits, over tiles of half the size.  (Rows with a
-// scale each keep to the 32-bit instruction and its order of sums.)
+// are all that they have, and the products are three of the bf16 instruction, sixteen times as fast as that of 32 bits, over tiles of half the size.  (us, the 32-bit instruction / three
+// parts, eight key heads of four, d = 128, fp8 in blocks: 200 tokens over 500 to 1500 keys 366 / 123, a token over 30000 66.5 / 29.6, 32 x 8 drafts over 300 to 2000 103 / 50, 1000 rows
+// over 2000 300 / 107, two sequences of 700 over 8000 1678 / 473.  Rows with a scale each keep to the 32-bit instruction and its order of sums.)
 template <typename T, int FORM> constexpr bool in_thirds() { return sizeof(T) == 4 && in_blocks(FORM); }
 template <typename T, int FORM> using TileType = std::conditional_t<in_thirds<T, FORM>(), uint16_t, T>;   // of a tile's values in the LDS
 
@@ -279,15 +280,30 @@ __device__ __forceinline__ void add_values_twice(const unsigned char *vt, const 
 template <typename L, int D, int PITCH>
 __device__ __forceinline__ void add_values_in_thirds(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32])
 {
-    float part[3][16];
+    const int i = lane & 15, hh = lane >> 5;
+    const unsigned char *at = vt + (4 * hh + (i >> 2)) * PITCH + L::value_at(lane);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float x[3];
-        cut_in_thirds(p[i], x);
-        part[0][i] = x[0]; part[1][i] = x[1]; part[2][i] = x[2];
+    for (int s = 0; s < 2; ++s) {
+        float part[8][3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cut_in_thirds(p[8 * s + e], part[e]);
+        union { uint4 u; bf16x8 v; } w[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            w[k].u = make_uint4(pack_bf16(part[0][k], part[1][k]), pack_bf16(part[2][k], part[3][k]), pack_bf16(part[4][k], part[5][k]), pack_bf16(part[6][k], part[7][k]));
+        bf16x8 v[D / 32];
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            typedef __attribute__((address_space(3))) bf16x4 lds4;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + 16 * s * PITCH + L::block_at(b)));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(at + (16 * s + 8) * PITCH + L::block_at(b)));
+            v[b] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+#pragma unroll
+        for (int k = 2; k >= 0; --k)
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[b], w[k].v, o[b], 0, 0, 0);
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) add_values<L, D, PITCH>(vt, pack_weights(part[k]), lane, o);
 }
 template <typename L, int D, int PITCH>
 __device__ __forceinline__ void add_values(const unsigned char *vt, const float (&p)[16], int lane, f32x16 (&o)[D / 32], float)

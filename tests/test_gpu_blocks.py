@@ -231,6 +231,48 @@ def test_attention_scalar_kernel(dtype, form):
 
 
 @pytest.mark.parametrize("impl", IMPLS)
+@pytest.mark.parametrize("form", mu.BLOCKS)
+@pytest.mark.parametrize("pairs", [[(1, 300), (3, 90)], [(60, 300), (40, 90)]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_large_and_small_numbers(form, impl, pairs, d):
+    """Queries and keys of 32 bits far from 1, whose products are not; values of all sizes."""
+    say(f"large and small numbers form={form} impl={impl} {pairs} d={d}")
+    for query, key, value, scale in ((100, -70, 90, -30), (-60, 60, -60, 0), (0, -95, 0, 95), (40, 40, 60, -80)):
+        b = mu.Batch(pairs, H=2, G=2, d=d, ps=32, block=16, dtype=gk.FP32, form=form, impl=impl, before=1, behind=1, seed=query + 100)
+        for n, e in (("K", key), ("V", value)):
+            x = b.values(n)
+            b.set_pool(n, (x / x.abs().max() * 2.0 ** e * 3).float())
+        Q = b.random_rows(4) * 2.0 ** query
+        b.p.softmax_scale = 2.0 ** scale / math.sqrt(d)
+        out, lse = run_attend(b, Q)
+        pu.check_attend(b, Q, out, lse, scale=2.0 ** scale / math.sqrt(d))
+
+
+@pytest.mark.parametrize("impl", IMPLS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", mu.BLOCKS)
+@pytest.mark.parametrize("pairs", [[(1, 300), (3, 90)], [(60, 300), (40, 90)]])
+def test_attention_of_queries_that_are_no_numbers(dtype, form, impl, pairs):
+    """Infinities of both signs and NaN of any bits in a query: NaN in its output, the others' bits as without."""
+    say(f"queries that are no numbers dtype={dtype} form={form} impl={impl} {pairs}")
+    b = mu.Batch(pairs, H=2, G=2, d=128, ps=32, block=16, dtype=dtype, form=form, impl=impl)
+    Q = b.random_rows(4)
+    want, want_lse = run_attend(b, Q)
+    odd = [math.inf, -math.inf, math.nan]
+    if dtype == gk.FP32:
+        odd.append(torch.tensor([0x7f800001], dtype=torch.int32).view(torch.float32))   # (all but the last of its bits are an infinity's)
+    for i, x in enumerate(odd):
+        for r, h, c in ((0, 1, 5), (b.rows - 1, 3, 127), (2, 0, 0)):
+            T = Q.clone()
+            T[r, h, c] = x
+            out, lse = run_attend(b, T)
+            assert out[r, h].isnan().all() and lse[r, h].isnan()
+            rest = torch.ones(b.rows, 4, dtype=torch.bool)
+            rest[r, h] = False
+            assert torch.equal(bits(out.cpu()[rest]), bits(want.cpu()[rest])) and torch.equal(bits(lse.cpu()[rest]), bits(want_lse.cpu()[rest]))
+
+
+@pytest.mark.parametrize("impl", IMPLS)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("form", mu.BLOCKS)
 def test_attention_over_blocks_without_a_scale(dtype, form, impl):
