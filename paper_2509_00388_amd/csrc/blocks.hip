@@ -5,10 +5,10 @@
 // rounded again, round(code * old / new): a power of two apart for e4m3, in 64 bits for integers.
 //
 // A wave or a workgroup takes a block of a head: the largest magnitude of its new rows, then their codes; rows stay in registers between the two where
-// they are few enough, else they are read again.  Which block it is follows from the blocks that the sequences before have new rows in: a lane counts
-// a sequence's.  Bound by memory where rows are many: 20000 bf16 rows of eight heads of 128 to fp8 in blocks of 64 in 28 us, 4.4 TB/s; 2055 fp32 rows of
+// they are few enough, else they are read again.  Which block it is follows from the row numbers: the room for blocks that the sequences before have
+// ascends with them, so that votes find the sequence.  Bound by memory where rows are many: 20000 bf16 rows of eight heads of 128 to fp8 in blocks of 64 in 28 us, 4.4 TB/s; 2055 fp32 rows of
 // sixteen heads of 64 to int8 in blocks of 16 in 11 us, a round of waves; a token each of 64 sequences in 4.2 us, a chain of look-ups and loads.  Blocks found from rows that
-// begin one cost 64 sequences of 8 rows 10.7 us of a call where these cost 6.8, of 64 rows in blocks of 128 76 and 12.5.
+// begin one cost 64 sequences of 8 rows 10.7 us of a call where these cost 7.2; from counts of the sequences before, 2000 sequences of a row 44 instead of 17.
 #include "kernels.hpp"
 #include "paged.hpp"
 
@@ -65,7 +65,7 @@ struct BlocksWrite {
     long row_stride, head_stride;
     void *Kpages, *Vpages;
     float *Kscale, *Vscale;
-    int group;   // lanes of a row
+    int group, by_row;   // lanes of a row; room for blocks: one a row, or rows / tokens + 2 a sequence
 };
 
 // A block of a head is WAVES waves' work: of one, so that four heads share a workgroup, or of all four.  HELD: pieces of each tensor that a thread
@@ -82,32 +82,25 @@ __global__ __launch_bounds__(256) void blocks_write_kernel(PagedBatch b, BlocksW
     const int tokens = 1 << b.scale_shift;
     const T *K = reinterpret_cast<const T *>(w.K) + h * w.head_stride, *V = reinterpret_cast<const T *>(w.V) + h * w.head_stride;
 
-    // Block number blockIdx.x of those with new rows: a lane counts those of a sequence, 64 sequences at a time (four a lane are no faster).
-    uint32_t number = blockIdx.x;
-    int s = 0, row0 = 0, lo = 0, len = 0, which = -1;   // sequence, row of its position 0 (were it there), new positions, which of its blocks
-    for (int from = 0; from < b.n_seqs; from += kWave) {
-        const int x = from + lane;
-        SeqRows q{0, 0, 0};
-        if (x < b.n_seqs) q = seq_rows(b, x);
-        const int start = max(q.len - q.n, 0);   // (more rows than the sequence is long: the first have no place)
-        const uint32_t has = q.n > 0 && q.len > 0 ? ((q.len - 1) >> b.scale_shift) - (start >> b.scale_shift) + 1 : 0;
-        const uint32_t incl = wave_scan_op(has, 0u, [](uint32_t l, uint32_t r) { return l + r; });
-        const uint64_t above = __ballot(incl > number);
-        if (above == 0) {
-            number -= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
-            continue;
-        }
-        const int l = __builtin_ctzll(above);
-        auto of_lane = [l](int v) { return __builtin_amdgcn_readlane(v, l); };
-        s = from + l;
-        row0 = of_lane(q.row0 + q.n - q.len);
-        lo = of_lane(start);
-        len = of_lane(q.len);
-        which = (int)(number - (uint32_t)of_lane((int)(incl - has)));
-        break;
-    }
-    // (The grid has room for blocks that a sequence may begin in their middle; sums of row numbers that do not ascend may pass 32 bits.)
-    if (which < 0 || which > ((len - 1) >> b.scale_shift) - (lo >> b.scale_shift)) return;
+    // Each sequence has room for as many blocks as its rows may lie in, and this is one of them.
+    const int number = blockIdx.x;
+    auto room_to = [&](int s) {   // of all sequences up to s
+        const int rows = min(max(b.row_start[s + 1], 0), b.n_rows);
+        return w.by_row ? rows : (rows >> b.scale_shift) + 2 * (s + 1);
+    };
+    int s = 0, among = b.n_seqs;
+    narrow_down(s, among, lane, [&](int x) { return room_to(x) <= number; });
+    if (among == 0) return;
+    const int x = s + min(lane, among - 1);
+    const SeqRows q = seq_rows(b, x);
+    const int l = (int)__popcll(__ballot(lane < among && room_to(x) <= number));
+    if (l >= among) return;
+    auto of_lane = [l](int v) { return __builtin_amdgcn_readlane(v, l); };
+    s += l;
+    const int q_row0 = of_lane(q.row0), n = of_lane(q.n), len = of_lane(q.len), which = number - (w.by_row ? q_row0 : (q_row0 >> b.scale_shift) + 2 * s);
+    // (more rows than the sequence is long: the first have no place)
+    const int lo = max(len - n, 0), row0 = q_row0 + n - len;   // the first new position, the row of position 0, were it there
+    if (n <= 0 || len <= 0 || which < 0 || which > ((len - 1) >> b.scale_shift) - (lo >> b.scale_shift)) return;
     const int begin = ((lo >> b.scale_shift) + which) << b.scale_shift;   // the block's first position
     const int pos = max(begin, lo), inside = pos - begin, rest = min(begin + tokens, len) - pos, first = row0 + pos;
     const int page = raw_page(b, s, pos);
@@ -197,13 +190,14 @@ hipError_t launch_blocks_write(const PagedBatch &b, int dtype, int form, const v
     const int pieces = b.d / (dtype == 0 ? 4 : 8);
     int group = 1;
     while (group < pieces && group < kWave) group <<= 1;
-    const BlocksWrite w{K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, group};
     const int tokens = 1 << b.scale_shift, most = b.max_rows < tokens ? b.max_rows : tokens;   // new rows of a block
     const int at_once = kWave / group;   // rows that a wave takes at once
     const bool one_wave = most <= 8 * at_once;   // (400 rows of 128 bf16: blocks of 32 in 9.9 us by a wave, 13.3 by four; of 64, twice as many turns, 22.2 and 12.6)
     // n rows of a sequence lie in (n - 2) / tokens + 2 blocks at most, and in n.
     const long blocks = b.n_rows / tokens + 2l * b.n_seqs;
-    const dim3 grid(blocks < b.n_rows ? (int)blocks : b.n_rows, one_wave ? (b.H + 3) / 4 : b.H);
+    const int by_row = blocks >= b.n_rows;
+    const BlocksWrite w{K, V, row_stride, head_stride, Kpages, Vpages, Kscale, Vscale, group, by_row};
+    const dim3 grid(by_row ? b.n_rows : (int)blocks, one_wave ? (b.H + 3) / 4 : b.H);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(b, w); return hipGetLastError(); };
     auto with_size = [&](auto type, auto f) {
         using T = decltype(type);

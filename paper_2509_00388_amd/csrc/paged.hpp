@@ -32,18 +32,25 @@ __device__ __forceinline__ SeqRows seq_rows(const PagedBatch &b, int s)
     return {r0, min(r1 - r0, b.max_rows), min(max(b.seq_len[s], 0), b.table_pages << b.page_shift)};
 }
 
+// The first of the n sequences from lo on of which ends(s) is false (the same in all lanes of the wave), where ends(s) ascends from true to false; at most
+// 64 are left for the caller's lanes to look at: lo and n are narrowed down by votes, each of which leaves a 64th.
+template <typename F> __device__ __forceinline__ void narrow_down(int &lo, int &n, int lane, F ends)
+{
+    while (n > kWave) {
+        const int piece = (n + kWave - 1) / kWave, last = lo + min((lane + 1) * piece, n) - 1;   // the last of the lane's piece
+        const int ended = (int)__popcll(__ballot(ends(last)));
+        lo += min(ended * piece, n);
+        n = min(piece, max(n - ended * piece, 0));
+    }
+}
 // The sequence that owns a row (the same in all lanes of the wave), n_seqs if none does.  Row numbers ascend, so it is the
-// number of sequences that end at or before the row: a vote of 64 at a time.
+// number of sequences that end at or before the row.
 __device__ __forceinline__ int seq_of_row(const PagedBatch &b, int row, int lane)
 {
-    int s = 0;
-    for (int first = 0; first < b.n_seqs; first += kWave) {
-        const int i = first + lane;
-        const int ended = (int)__popcll(__ballot(i < b.n_seqs && b.row_start[min(i, b.n_seqs - 1) + 1] <= row));
-        s += ended;
-        if (ended < kWave) break;
-    }
-    return s;
+    int lo = 0, n = b.n_seqs;
+    auto ends = [&](int s) { return b.row_start[s + 1] <= row; };
+    narrow_down(lo, n, lane, ends);
+    return lo + (int)__popcll(__ballot(lane < n && ends(lo + lane)));
 }
 
 // Number of the pool's row that holds head 0 of position pos (0 <= pos < tokens of the table) of a sequence, -1 where the
