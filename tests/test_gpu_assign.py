@@ -57,7 +57,8 @@ class Turn:
 
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("n_seqs,ps,most", [(1, 16, 400), (3, 1, 9), (64, 16, 700), (200, 4, 60), (256, 128, 900), (257, 16, 100), (1000, 16, 70),
-                                            (1024, 2, 9), (1025, 16, 80), (2500, 8, 50)])
+                                            (1024, 2, 9), (1025, 16, 80), (2500, 8, 50), (2048, 16, 40), (2049, 16, 20), (4096, 4, 12),
+                                            (3000, 4, 90), (4097, 16, 30), (9000, 8, 20)])
 def test_turns(n_seqs, ps, most, in_place):
     """Turns of a scheduler: prompts, single tokens, drafts, sequences that are cut or end, pages that run out."""
     say(f"turns n_seqs={n_seqs} ps={ps} in_place={in_place}")
@@ -85,7 +86,7 @@ def test_taken_back():
     assert torch.equal(again[1], grown[1]) and torch.equal(again[6], grown[6])
 
 
-@pytest.mark.parametrize("n_seqs", [40, 1500])
+@pytest.mark.parametrize("n_seqs", [40, 1500, 4000, 5000])
 def test_refusals(n_seqs):
     """Sequences that ask for more than their table, max_rows, the rows or the free pages hold; later ones that ask for less."""
     say(f"refusals n_seqs={n_seqs}")
@@ -116,7 +117,7 @@ def test_arrays_of_any_content():
     """Lengths, page numbers and counts outside their ranges: nothing outside the arrays is touched, and what is stated holds."""
     say("arrays of any content")
     worst = [-2 ** 31, -1, 0, 1, 2 ** 30, 2 ** 31 - 1]
-    for n_seqs in (6, 1030):
+    for n_seqs in (6, 1030, 3000, 4100):
         t = Turn([20] * n_seqs, 4, 9, spare=50, seed=n_seqs)
         t.had = [worst[s % 6] for s in range(n_seqs)]
         keep = [worst[(s // 2) % 6] for s in range(n_seqs)]
@@ -148,7 +149,7 @@ def test_nothing_to_assign():
     assert length.numel() == 0 and after.tolist() == [4] and start.tolist() == [0] and (pos == -1).all()
 
 
-@pytest.mark.parametrize("n_seqs", [50, 1400])
+@pytest.mark.parametrize("n_seqs", [50, 1400, 2100, 4500])
 def test_captured_turns(n_seqs):
     """A captured turn, replayed with other lengths, with eager work between: the state that the definition gives."""
     say(f"captured turns n_seqs={n_seqs}")
