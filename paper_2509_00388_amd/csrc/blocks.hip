@@ -202,6 +202,7 @@ hipError_t launch_blocks_write(const PagedBatch &b, int dtype, int form, const v
     auto with_size = [&](auto type, auto f) {
         using T = decltype(type);
         constexpr int FORM = decltype(f)::value;
+        // (pieces held, one / eight, us of a call: 64 sequences of a row 5.8 / 6.4, 2000 17.2 / 26.2)
         return most <= at_once ? go(blocks_write_kernel<T, FORM, 1, 1>)
              : one_wave        ? go(blocks_write_kernel<T, FORM, 1, 8>) : go(blocks_write_kernel<T, FORM, 4, 4>);
     };
