@@ -395,7 +395,7 @@ bool plan_attend(const graphkv_paged_params *p, AttendPlan &A, bool cross = fals
         A.total = A.few_slots + align_up(join_slot_bytes(A.fp.join));
     }
     if (A.many) {
-        A.mp = many_plan(b, p->dtype, A.G, A.few);
+        A.mp = many_plan(b, p->dtype, p->page_format, A.G, A.few, cross);
         if (A.mp.join.n_wg == 0) return false;
         A.many_records = A.total;
         A.many_slots = A.many_records + align_up(join_record_bytes(A.mp.join));

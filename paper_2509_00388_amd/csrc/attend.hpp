@@ -128,6 +128,7 @@ struct ManyPlan {
     int leave_few;    // sequences of few rows are the other kernel's
     int wide;         // blocks of 256 rows (attend_wide.hpp)
     int single;       // a block has one unit: none is split
+    uint32_t half_to;   // so many units and fewer are shared among one workgroup a compute unit
 };
 struct ManySeq {
     int rows, blocks;        // stacked
@@ -199,7 +200,7 @@ __device__ __forceinline__ bool next_part(const AttendArgs &a, const ManyPlan &p
 // ---- launchers ------------------------------------------------------------------------------------------
 bool attend_mfma_applies(int dtype, int d);   // whether the matrix-core kernels take this head dimension
 FewPlan few_plan(const PagedBatch &b, int dtype, int form, int G, bool cross);
-ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few);   // no workgroups: more units than 31 bits count
+ManyPlan many_plan(const PagedBatch &b, int dtype, int form, int G, bool leave_few, bool cross);   // no workgroups: more units than 31 bits count
 hipError_t launch_attend_generic(const AttendArgs &a, int dtype, int form, bool cross, hipStream_t st);
 // (`cross`: rows see all of their sequence.  The kernels of each kind are compiled in files of their own: these, blocks_attend.hip, cross_*.hip.)
 hipError_t launch_attend_few(const AttendArgs &a, const FewPlan &pl, int dtype, int form, bool cross, hipStream_t st);

@@ -3,7 +3,7 @@
 
 namespace gkv {
 
-ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
+ManyPlan many_plan(const PagedBatch &b, int dtype, int form, int G, bool leave_few, bool cross)
 {
     const int D = attend_width(b.d);
     ManyPlan p{};
@@ -36,6 +36,11 @@ ManyPlan many_plan(const PagedBatch &b, int dtype, int G, bool leave_few)
     p.single = cap <= (long)p.tile_keys * p.step;
     const int most = p.wide ? 256 : 512;   // one or two workgroups a compute unit
     p.join.n_wg = units > INT32_MAX ? 0 : units < most ? (int)units : most;
+    // Few blocks in many parts keep the joining launch waiting: where their keys are not many, which the device finds out, half the workgroups do.  (us, 512 /
+    // 256, one sequence of 16 rows over 20000 keys, four heads of seven 51.1 / 38.5, eight of four 45.8 / 40.8, with 32-bit rows over other states 58.5 / 44.9, 56.1 / 53.7; one of
+    // 30 over 10000 43.2 / 34.0, two of 12 over 8000 43.2 / 29.0; but two of 16 over 40000 64.3 / 70.7, with 32-bit rows 124 / 151, and with more blocks 20 of 16 over 300 to
+    // 900 29.0 / 31.4.  Causal attention over pages of rows keeps the order of its sums.)
+    if ((cross || in_blocks(form)) && blocks * b.H <= 32) p.half_to = 163840u >> p.unit_shift;
     return p;
 }
 
