@@ -378,9 +378,9 @@ int32_t graphkv_cache_read(const graphkv_paged_params *p, const void *Kpages, co
  * graphkv_attend_workspace_bytes() is 0 for params that are refused, and where no scratch
  * memory is needed: by the scalar kernel, and without rows or sequences.
  * Softmax statistics and sums are held in 32 bits.  With bf16 rows the weights (times the
- * values' scales, of 8-bit pages) are rounded to bf16 for the product with the values; where the kernel
- * for few rows reads plain pages, to two bf16 numbers each, which keep 15 bits.  (With pages in blocks a weight and the scale of its value are one
- * exponential, whose argument is rounded to 32 bits.)  With fp32 rows none is rounded to fewer than 24 bits; over pages in blocks,
+ * values' scales, of 8-bit pages) are rounded to bf16 for the product with the values, where what is below 2^-126 may be
+ * lost; where the kernel for few rows reads plain pages, to two bf16 numbers each, which keep 15 bits.  The sums of the softmax
+ * are of the weights as they were before.  With fp32 rows none is rounded to fewer than 24 bits; over pages in blocks,
  * of queries, and of weights times scales, what is below 2^-126 may be lost (queries or values of less than 2^-70 have fewer than 24 bits then).  (Sums of values
  * beyond 2^100 may leave the range of 32 bits.)  A row that sees nothing, or
  * nothing but logits of -infinity, has out = 0 and lse = -infinity.  What lies in places that a row does not see (later

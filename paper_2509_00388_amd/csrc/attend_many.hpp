@@ -22,9 +22,8 @@ namespace gkv {
 
 namespace {
 
-// Bytes of a tile's scales in the LDS: two a key, or three for each group of 16 keys (the scale of its keys, and of its values as
-// softmax_blocks() takes it).
-constexpr int scale_bytes(int form, int keys) { return form == kPagesPlain ? 0 : in_blocks(form) ? 64 : 2 * keys * 4; }
+// Bytes of a tile's scales in the LDS: two a key, or two for each of up to four groups of 16 keys.
+constexpr int scale_bytes(int form, int keys) { return form == kPagesPlain ? 0 : in_blocks(form) ? 32 : 2 * keys * 4; }
 
 // Bytes of the third part of a wave's queries in the LDS (attend_many.inc).
 template <int D> constexpr int kThirdBytes = 32 * (2 * D + 16);

@@ -1,0 +1,88 @@
+"""Attention over pages of 8-bit codes with a scale a block: scales of every size, against the definition in 64 bits (GPU)."""
+import math
+
+import pytest
+import torch
+
+from paper_2509_00388_amd import binding as gk
+from tests import more_util as mu
+from tests.test_gpu_cross import run_cross
+from tests.test_gpu_paged import run_attend, say
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [gk.BF16, gk.FP32]
+# the kernels for few rows, for blocks of 64 and of 128 of them, and for blocks of 256
+PAIRS = [[(1, 300), (3, 90)], [(12, 300), (20, 90)], [(60, 300), (40, 90)], [(70, 300), (3, 90)]]
+
+
+def run(b, Q):
+    return (run_cross if b.cross else run_attend)(b, Q)
+
+
+def check(want, out, lse):
+    """What pu.check_attend checks, with a definition that is there already."""
+    value, _, bound, _ = want
+    mine = ~value.isnan()
+    out, lse = out.double().cpu(), lse.double().cpu()
+    assert torch.isfinite(out[mine]).all()
+    assert ((out - value).abs() <= bound + 2.0 ** -100)[mine].all()
+    check_lse(want, lse)
+
+
+def check_lse(want, lse):
+    _, log_sum, _, lse_bound = want
+    lse = lse.double().cpu()
+    none = log_sum == -math.inf
+    assert (lse[none] == -math.inf).all()
+    assert ((lse - log_sum).abs() <= lse_bound)[~log_sum.isnan() & ~none].all()
+
+
+def some_blocks(b, share):
+    """A choice among all blocks of the pool, [pages, heads, blocks of a page]."""
+    return torch.rand(b.p.n_pages, b.H, b.ps // b.block, generator=b.g) < share
+
+
+def sized(b, n, exponents):
+    """The pool's rows with a power of two a block, of these."""
+    e = torch.tensor(exponents)[torch.randint(0, len(exponents), (b.p.n_pages, b.H, b.ps // b.block), generator=b.g)].double()
+    size = torch.exp2(e).repeat_interleave(b.block, 2)[..., None]
+    x = b.values(n)
+    b.set_pool(n, (x / x.abs().amax() * size).to(b.p.torch_dtype))
+
+
+@pytest.mark.parametrize("cross", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", mu.BLOCKS)
+@pytest.mark.parametrize("pairs", PAIRS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_scales_of_values_that_are_zero(cross, dtype, form, pairs, d):
+    """A block of codes that are 0 adds nothing to the output and its weights to the sum, whatever its scale is."""
+    say(f"scales of values that are zero cross={cross} dtype={dtype} form={form} {pairs} d={d}")
+    b = mu.Batch(pairs, cross=cross, H=2, G=2, d=d, ps=32, block=16, dtype=dtype, form=form, before=1, behind=1, spare=3, seed=d)
+    zero = some_blocks(b, 0.5)
+    b.pool["V"].view(torch.uint8)[zero.repeat_interleave(b.block, 2)] = 0
+    Q = b.random_rows(4)
+    want = b.attend(Q)
+    for scale in (0.0, 2.0 ** -149, 2.0 ** -130, 2.0 ** -126, 2.0 ** -108, 2.0 ** -60, 2.0 ** 60, 2.0 ** 100):
+        b.pool["Vs"][zero] = scale
+        check(want, *run(b, Q))
+
+
+@pytest.mark.parametrize("cross", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", mu.BLOCKS)
+@pytest.mark.parametrize("pairs", PAIRS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_of_all_sizes(cross, dtype, form, pairs, d):
+    """Blocks of values next to nothing and of large ones beside others; the logarithm of the sum does not depend on them."""
+    say(f"values of all sizes cross={cross} dtype={dtype} form={form} {pairs} d={d}")
+    for exponents in ((0, -90, -95, -99), (-90, -99), (0, 20, 33, -33, -20), (0, 60, 90, -60), (119, 0, 127)):
+        b = mu.Batch(pairs, cross=cross, H=2, G=2, d=d, ps=32, block=16, dtype=dtype, form=form, before=1, behind=1, seed=d)
+        sized(b, "V", exponents)
+        Q = b.random_rows(4)
+        want, got = b.attend(Q), run(b, Q)
+        if max(exponents) > 100:      # (sums of such values may leave the range of 32 bits)
+            check_lse(want, got[1])
+        else:
+            check(want, *got)
