@@ -446,8 +446,13 @@ __device__ __forceinline__ void softmax_groups(f32x16 (&x)[NB], const float *ks,
     }
     softmax_blocks<NB, DB>(x, kc, vs, all, seen, hh, m, l, o, p);
 }
-// A keys' scale as those need it: 0, which a block of zeros has, counts as 1.
-__device__ __forceinline__ float not_zero(float scale) { return scale == 0.f ? 1.f : scale; }
+// A keys' scale times c as those need it, above 0: it multiplies the logits of hidden keys too, -infinity.  What is 0, in a block of zeros or next to it, becomes the least number:
+// logits are off by 2^-21 then at most.
+__device__ __forceinline__ float key_scale(float scale, float c)
+{
+    const float k = scale * c;
+    return k == 0.f ? 0x1p-149f : k;
+}
 
 // The weights times the values' scales vs; keys that the lane does not see keep weight 0, whatever their scale.
 template <int NB>

@@ -86,3 +86,19 @@ def test_values_of_all_sizes(cross, dtype, form, pairs, d):
             check_lse(want, got[1])
         else:
             check(want, *got)
+
+
+@pytest.mark.parametrize("cross", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", mu.BLOCKS)
+@pytest.mark.parametrize("pairs", PAIRS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_next_to_nothing(cross, dtype, form, pairs, d):
+    """Scales of keys whose product with the softmax scale is below every number of 32 bits: all keys that a row sees weigh the same."""
+    say(f"logits next to nothing cross={cross} dtype={dtype} form={form} {pairs} d={d}")
+    for exponents, scale in (((-99,), 2.0 ** -60), ((-99, 0), 2.0 ** -60), ((-90, 0), 2.0 ** -30)):
+        b = mu.Batch(pairs, cross=cross, H=2, G=2, d=d, ps=32, block=16, dtype=dtype, form=form, before=1, behind=1, seed=d)
+        sized(b, "K", exponents)
+        b.p.softmax_scale = scale
+        Q = b.random_rows(4)
+        check(b.attend(Q, scale), *run(b, Q))
