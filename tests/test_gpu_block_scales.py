@@ -6,8 +6,9 @@ import torch
 
 from paper_2509_00388_amd import binding as gk
 from tests import more_util as mu
+from tests import paged_util as pu
 from tests.test_gpu_cross import run_cross
-from tests.test_gpu_paged import run_attend, say
+from tests.test_gpu_paged import bits, run_attend, say
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +103,36 @@ def test_logits_next_to_nothing(cross, dtype, form, pairs, d):
         b.p.softmax_scale = scale
         Q = b.random_rows(4)
         check(b.attend(Q, scale), *run(b, Q))
+
+
+@pytest.mark.parametrize("cross", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pairs", PAIRS)
+@pytest.mark.parametrize("d", [48, 64, 80, 96, 112, 128, 160, 192, 240])
+def test_values_that_are_no_numbers_stay_in_their_column(cross, dtype, pairs, d):
+    """NaN in one column of early values, which all rows see, over several tiles: NaN in that column alone, everything else as without."""
+    say(f"NaN in a column cross={cross} dtype={dtype} {pairs} d={d}")
+    b = mu.Batch(pairs, cross=cross, H=2, G=2, d=d, ps=32, block=16, dtype=dtype, form=gk.PAGES_FP8_BLOCKS, before=1, behind=1, seed=d)
+    Q = b.random_rows(4)
+    clean, clean_lse = run(b, Q)
+    pu.check_attend(b, Q, clean, clean_lse)
+    code = b.pool["V"].view(torch.uint8).clone()
+    # (a tile of keys that some rows do not see all of takes such values apart from the product, with weights of 32 bits)
+    tile = 256 if d <= 64 else 128
+    early = [n if cross else (n - new + 1) // tile * tile for new, n in pairs]
+    assert early[0] >= 128 or max(n for n, _ in pairs) > 1
+    owner = torch.full((b.rows,), -1)
+    for r, s, _ in b.each_row():
+        owner[r] = s
+    for column in sorted({0, 5, 20, d // 2, d - 9, d - 1}):
+        b.pool["V"].view(torch.uint8).copy_(code)
+        for s, n in enumerate(early):
+            for j in range(min(n, 140)):
+                page, at = b.place(s, j)
+                b.pool["V"].view(torch.uint8)[page, :, at, column] = 0x7f
+        out, lse = run(b, Q)
+        assert torch.equal(bits(lse), bits(clean_lse)), column
+        rest = [c for c in range(d) if c != column]
+        assert torch.equal(out[:, :, rest], clean[:, :, rest]), column
+        for s, n in enumerate(early):
+            assert out[(owner == s).cuda()][:, :, column].isnan().all() == (n > 0), (column, s)
