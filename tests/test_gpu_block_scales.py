@@ -1,4 +1,5 @@
-"""Attention over pages of 8-bit codes with a scale a block: scales of every size, against the definition in 64 bits (GPU)."""
+"""Attention over pages of 8-bit codes with a scale a block: scales of every size, few blocks of rows over many keys, large pools, against the
+definition in 64 bits (GPU)."""
 import math
 
 import pytest
@@ -7,6 +8,7 @@ import torch
 from paper_2509_00388_amd import binding as gk
 from tests import more_util as mu
 from tests import paged_util as pu
+from tests.test_gpu_blocks import dense_check
 from tests.test_gpu_cross import run_cross
 from tests.test_gpu_paged import bits, run_attend, say
 
@@ -136,3 +138,50 @@ def test_values_that_are_no_numbers_stay_in_their_column(cross, dtype, pairs, d)
         assert torch.equal(out[:, :, rest], clean[:, :, rest]), column
         for s, n in enumerate(early):
             assert out[(owner == s).cuda()][:, :, column].isnan().all() == (n > 0), (column, s)
+
+
+# 257 to 640 units of 256 keys of a single block of up to 64 rows a head: half of the workgroups share them
+FEW_BLOCKS = [([(16, 20000)], 8, 4, 64), ([(30, 10000)], 8, 2, 128), ([(12, 8000), (12, 9000)], 8, 4, 64), ([(16, 39000)], 4, 4, 128)]
+
+
+@pytest.mark.parametrize("cross,form", [(False, gk.PAGES_FP8_BLOCKS), (True, gk.PAGES_INT8_BLOCKS), (True, gk.PAGES_PLAIN), (True, gk.PAGES_FP8)])
+@pytest.mark.parametrize("shape", range(len(FEW_BLOCKS)))
+def test_few_blocks_over_many_keys(cross, form, shape):
+    pairs, H, G, d = FEW_BLOCKS[shape]
+    say(f"few blocks over many keys cross={cross} form={form} {FEW_BLOCKS[shape]}")
+    b = mu.Batch(pairs, cross=cross, H=H, G=G, d=d, ps=64, block=32, form=form, seed=shape, before=1, behind=1)
+    units = sum(-(-n // 256) for _, n in pairs) * H
+    assert 256 < units <= 640
+    Q = b.random_rows(H * G)
+    out, lse = run(b, Q)
+    dense_check(b, Q, out, lse)
+
+
+@pytest.mark.parametrize("form", mu.BLOCKS)
+@pytest.mark.parametrize("dtype,d", [(gk.BF16, 256), (gk.BF16, 128), (gk.FP32, 128)])
+def test_places_beyond_two_gigabytes(form, dtype, d):
+    """Codes of the pool's last pages, more than 2^31 bytes behind its begin, by every kernel, against the definition."""
+    say(f"places beyond two gigabytes form={form} dtype={dtype} d={d}")
+    H, ps, block = 2, 1024, 64
+    pages = (1 << 31) // (H * ps * d) + 6
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    pools = [torch.zeros(pages, H, ps, d, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(pages, H, ps // block, device="cuda") for _ in range(2)]
+    for cross in (False, True):
+        for pairs in ([(1, 1500), (3, 700)], [(20, 1500), (12, 700)], [(150, 1300), (3, 700)]):
+            b = mu.Batch(pairs, cross=cross, H=H, G=2, d=d, ps=ps, block=block, dtype=dtype, form=form, before=1, behind=1, seed=d)
+            n = b.p.n_pages
+            for i, name in enumerate("KV"):      # the batch's own few pages become the last of the large pools
+                pools[i][-n:] = b.pool[name].view(torch.uint8).cuda()
+                scales[i][-n:] = b.pool[name + "s"].cuda()
+            Q, p = b.random_rows(H * 2), b.p
+            want = b.attend(Q)
+            p.n_pages = pages
+            start, t = pages - n, b.pool["K"].dtype
+            assert start * H * ps * d >= 2 ** 31
+            table = b.table.cuda() + start
+            out = torch.full((b.rows, H * 2, d), -7.0, dtype=p.torch_dtype, device="cuda")
+            lse = torch.full((b.rows, H * 2), -7.0, device="cuda")
+            call = gk.graphkv_cross_attend if cross else gk.graphkv_attend
+            call(p, Q.cuda(), pools[0].view(t), pools[1].view(t), table, i32(*b.len.tolist()), i32(*b.start.tolist()), *scales, out=out, lse=lse)
+            check(want, out, lse)
