@@ -138,7 +138,7 @@ class PagedParams:
 
     @property
     def tokens_a_scale(self) -> int:
-        return (self.scale_tokens or min(32, self.page_tokens)) if self.page_format >= PAGES_FP8_BLOCKS else 1
+        return max(1, self.scale_tokens or min(32, self.page_tokens)) if self.page_format >= PAGES_FP8_BLOCKS else 1
 
 
 _lib = None

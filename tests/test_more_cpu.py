@@ -63,6 +63,14 @@ def test_a_scales_tokens_are_read_with_blocks_alone(lib):
     assert good(**{**BLOCK, "scale_tokens": 0, "page_tokens": 16}).c().scale_tokens == 16
 
 
+def test_pages_without_tokens_are_refused_as_other_params(lib):
+    """The binding counts the scales of a pool before the library sees the params."""
+    for kw in (dict(page_tokens=0), dict(page_tokens=0, scale_tokens=0), dict(page_tokens=-16, scale_tokens=0)):
+        p = good(**{**BLOCK, **kw})
+        assert p.tokens_a_scale > 0
+        assert set(calls(lib, p.c()).values()) == {-1}
+
+
 def test_pointers_and_workspace_are_checked(lib):
     for p in (good(), good(**BLOCK)):
         need = gk.graphkv_attend_workspace_bytes(p)
