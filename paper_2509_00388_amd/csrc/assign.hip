@@ -13,7 +13,7 @@
 // without the others' sums, leave theirs, and begin anew in the next launch: four of them, whatever the number.  Page numbers
 // and rows are dealt to the threads one by one, whoever's they are, and find their sequence in the sums, which lie in the LDS.  Few rows
 // are told their places in the same launch, many in one of their own.  Nothing but latency: a batch's numbers are a few kilobytes.  A token each of 64
-// sequences 4.0 us, 1000 sequences of which 111 end and are followed by prompts, 4400 pages that move and 126000 rows, 9.0 + 4.0, a prompt of 120000 rows
+// sequences 4.0 us, 1000 sequences of which 111 end and are followed by prompts, 4400 pages that move and 126000 rows, 9.4 + 4.0, a prompt of 120000 rows
 // 4.2 + 2.9; a call takes the host 9.
 #include "kernels.hpp"
 #include "paged.hpp"

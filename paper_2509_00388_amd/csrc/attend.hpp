@@ -110,7 +110,6 @@ struct JoinPlan {
 constexpr int kMostFewWorkgroups = 512;   // two a compute unit
 struct FewPlan {
     JoinPlan join;
-    int tile_keys;
     int whole;        // no pair is split: stretches are of pairs, and nothing is left to be joined
 };
 __device__ __forceinline__ bool has_few(const SeqRows &q, int G) { return q.n > 0 && q.n * (long)G <= kFewRows; }

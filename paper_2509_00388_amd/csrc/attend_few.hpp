@@ -9,7 +9,7 @@
 // in blocks).  A pair that one workgroup holds whole is finished there; the parts of others go to scratch memory and are joined by a second launch.
 //
 // Measured (bf16 rows, d = 128, eight key heads of four, the kernel alone): one token over 131072 keys 97 us, 5.5 TB/s (reading alone is faster than the 4.6 to 4.8 of
-// a copy); 64 tokens over 400 to 5000 keys each in fp8 pages 86 us, 4.5 TB/s, in blocks 80 us, 4.9; every pair that lies in two stretches costs
+// a copy); 64 tokens over 400 to 5000 keys each in fp8 pages 86 us, 4.5 TB/s, in blocks 80 to 83 us, 4.7 to 4.9; every pair that lies in two stretches costs
 // some 5 us, which is why 64 tokens over 2816 keys each, a pair a stretch, take 71 us in blocks and 63 of them 84; one token over 2048 keys 8.7 us, a chain of look-ups,
 // loads, two products and the join of the waves with a tile a workgroup.  States of d = 64, sixteen heads, 64 tokens over 200 to 1500 of them: 53 us, 4.2 TB/s.
 // Slower: three workgroups a compute unit, 768 or 1024 of them in all (in blocks too: 64 tokens over 4096 keys 101 -> 127), 64 keys a wave.

@@ -11,7 +11,7 @@
 // cubed reaches 1345, the kernel without its softmax took 850 us and without the reads of its operands from the LDS hardly less.  Slower, on one
 // card where the kernel took 1060 to 1095: 128 rows a workgroup and two of them 1290; a barrier between softmax and products that keeps the waves of a SIMD
 // half a tile apart 1090, with the operands' reads fixed by hand 1130, with tiles that pass the registers by (global_load_lds, pieces permuted
-// instead of padded) 1130.  In blocks of fp8 2000 rows over 24000 keys take 740 to 750 us (plain pages 755 to 765, fp8 with a scale a row 925 to 945); six sequences of 445
+// instead of padded) 1130.  In blocks of fp8 2000 rows over 24000 keys take 750 to 760 us (plain pages 755 to 765, fp8 with a scale a row 925 to 945); six sequences of 445
 // rows of two heads a group over 1000 to 9000 states 169, of which the parts of blocks that two workgroups share are 12 in the join and about as much
 // in the kernel (8 of 512 rows over 8192, a block a workgroup: 976 TFLOP/s).  Slower there: waves without rows that leave a tile out, with longer units for
 // blocks that are half full (182), units of one tile (185); a higher priority for the products' waves (822 for 745).

@@ -8,7 +8,7 @@
 // they are few enough, else they are read again.  Which block it is follows from the row numbers: the room for blocks that the sequences before have
 // ascends with them, so that votes find the sequence.  Bound by memory where rows are many: 20000 bf16 rows of eight heads of 128 to fp8 in blocks of 64 in 28 us, 4.4 TB/s; 2055 fp32 rows of
 // sixteen heads of 64 to int8 in blocks of 16 in 11 us, a round of waves; a token each of 64 sequences in 4.2 us, a chain of look-ups and loads.  Blocks found from rows that
-// begin one cost 64 sequences of 8 rows 10.7 us of a call where these cost 7.2; from counts of the sequences before, 2000 sequences of a row 44 instead of 17.
+// begin one cost 64 sequences of 8 rows 10.7 us of a call where these cost 6.8; from counts of the sequences before, 2000 sequences of a row 44 instead of 17.
 #include "kernels.hpp"
 #include "paged.hpp"
 
